@@ -71,11 +71,16 @@ enum {
     DELTA_OP_AVGPOOL = 2,    /* global average over H x W */
     DELTA_OP_SOFTMAX_CE = 3, /* mean cross-entropy of logits x [N, Cin] against labels `res` */
     DELTA_OP_ATTENTION = 4,  /* fused multi-head self-attention of a transformer layer (bf16, heads of 64) */
-    DELTA_OP_LAYERNORM = 5,  /* layer normalisation over the channel axis (bf16) */
+    DELTA_OP_LAYERNORM = 5,  /* layer normalisation over the channel axis */
     DELTA_OP_BATCHNORM = 6,  /* batch normalisation with the statistics of the batch (bf16) */
     DELTA_OP_RELU = 7,       /* y = max(x, 0) (bf16) */
-    DELTA_OP_ADD = 8         /* y = x + res (bf16) */
+    DELTA_OP_ADD = 8,        /* y = x + res (bf16) */
+    DELTA_OP_PACK8 = 9,      /* x into its checkpoint in 8 bits */
+    DELTA_OP_UNPACK8 = 10,   /* a checkpoint back into a tensor */
+    DELTA_OP_EMBEDDING = 11  /* rows of a table by token ids, times a factor */
 };
+/* Checkpoint formats (field `pack` of a layer). */
+enum { DELTA_PACK_NONE = 0, DELTA_PACK_INT8 = 1, DELTA_PACK_E4M3 = 2 };
 enum { DELTA_SYNC_D2H = 1, DELTA_SYNC_H2D = 2, DELTA_SYNC_COMPUTE = 4, DELTA_SYNC_ALL = 7 };
 enum { DELTA_DIR_D2H = 0, DELTA_DIR_H2D = 1, DELTA_DIR_BOTH = 2 };
 #define DELTA_NO_TENSOR 0xFFFFFFFFu
@@ -168,9 +173,21 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * [64 h, 64 h + 64) of each), y = ctx [N, H, Cout] = concat_h softmax(q_h k_h^T / 8) v_h over all H
  * positions, no mask; R = number of heads, Cout = 64 * R; the scores never reach memory (fp32 on
  * chip, probabilities rounded to bf16 before they multiply v).  W = S = stride = 1, pad = 0.
- * DELTA_OP_LAYERNORM: y = (x - mean) / sqrt(var + eps) * scale + shift over the Cin (= Cout,
- * multiple of 8, <= 2048) channels of each of the N*H*W rows; scale = gamma, shift = beta.
- * Both are bf16 only and ignore w and res.
+ * DELTA_OP_LAYERNORM: y = (x - mean) / sqrt(var + eps) * scale + shift over the Cin (= Cout) channels of each of
+ * the N*H*W rows, a multiple of 8 up to 2048 or a multiple of 64 up to 8192; scale = gamma, shift = beta (16-byte aligned).
+ * Attention is bf16 only, layer normalisation bf16 or fp32; both ignore w and take no res.
+ * DELTA_OP_EMBEDDING: y[m,k] = scale_k * w[id[m]][k] over m in N*H*W tokens (at most 16777216): x holds their ids, int64, Cin = the rows of
+ * the table (at most 4194303), Cout = its channels (a multiple of 8 up to 8192), w = the table [Cin][Cout] in the storage type, bf16 or fp32,
+ * scale = a factor per channel (a constant one for the usual sqrt(Cout)).  An id outside [0, Cin) stands for no token: its row of y is zero.
+ * Checkpoints in 8 bits (bf16 or fp32, Cin = Cout a multiple of 8): beside Evict and Offload a third way to make an activation small, to about a
+ * half (a quarter of fp32).  DELTA_OP_PACK8 writes y, the checkpoint of x over N*H*W rows of Cin channels; DELTA_OP_UNPACK8 restores a tensor from a
+ * checkpoint x; `pack` names the format, delta_packed_bytes the checkpoint's size.  A checkpoint is a tensor of the table like any other: it is released,
+ * offloaded and reloaded, and its parent in a graph is the tensor it was made from.  A row's channels go in blocks of 32 (the last of a row may be
+ * shorter); a block has one scale 2^e, e the smallest integer from -120 on for which no value of it exceeds 127 * 2^e (DELTA_PACK_INT8) or 448 * 2^e
+ * (DELTA_PACK_E4M3); a value is x / 2^e rounded, ties to even, to a whole number or to an OCP E4M3 number.  A block with an infinity or a NaN
+ * reads back as NaN throughout; what rounds up to 2^128 as an infinity.  What comes back is exact in bf16 and fp32, so a backward operator that reads the checkpoint works on the same
+ * values as one that reads the unpacked tensor.  Layout: N*H*W * Cin bytes (q in two's complement, or the E4M3 code), padded to 16; then e + 127 for each block,
+ * [row][block], padded to 16.
  * Operator granularity (the separate ConvForward / BNForward tensors of the paper's cost table,
  * Sec. 5.5; bf16 only, any N, H, W, Cin = Cout a multiple of 8): a bare convolution is
  * DELTA_OP_CONV with scale = ones, shift = zeros, relu = 0, no res.  DELTA_OP_BATCHNORM:
@@ -189,6 +206,8 @@ typedef struct {
     uint32_t op;               /* DELTA_OP_* */
     float eps;                 /* DELTA_OP_LAYERNORM and DELTA_OP_BATCHNORM */
     uint32_t fuse;             /* DELTA_FUSE_* bits (convolutions only; 0 everywhere else) */
+    uint32_t pack;             /* DELTA_PACK_*: the format of y (DELTA_OP_PACK8) or of x (DELTA_OP_UNPACK8; in a backward descriptor
+                                  also DELTA_OP_LAYERNORM and linear layers); 0 everywhere else */
 } delta_layer_desc;
 
 typedef struct {
@@ -206,7 +225,7 @@ typedef struct {
 
 /* Creates a context on the current HIP device.  arena_dev: device, 256-byte aligned,
  * arena_bytes long, or NULL for a planner-only context (then every call but delta_plan,
- * delta_last_error and delta_destroy fails with DELTA_ERR_STATE).  compute_stream: a
+ * delta_packed_bytes, delta_last_error and delta_destroy fails with DELTA_ERR_STATE).  compute_stream: a
  * hipStream_t (NULL = the default stream). */
 delta_status delta_create(void *arena_dev, uint64_t arena_bytes, void *compute_stream,
                           delta_ctx **out);
@@ -319,7 +338,7 @@ delta_status delta_set_skip_copies(delta_ctx *ctx, int32_t skip);
  * just those, and the data gradient is computed at the output's resolution and stored to
  * those pixels, zeros between, straight where the kernel that runs it can and nothing is added or masked; otherwise it goes into the workspace
  * first (delta_backward_kernel says "spread_add"), and gx_add is added in a second bf16 rounding.
- * Other operators (bf16 only; gpre must be gy, gx_add unused):
+ * Other operators (bf16 only, gpre must be gy, gx_add unused, unless said otherwise):
  *   DELTA_OP_MAXPOOL   gx receives gy routed to the first maximal element of each window (scan order
  *                      r, then s); needs fwd.x resident.  With mask_gx, gx is also multiplied by [x > 0].
  *   DELTA_OP_AVGPOOL   gx = gy / (H W) at every pixel.
@@ -332,6 +351,15 @@ delta_status delta_set_skip_copies(delta_ctx *ctx, int32_t skip);
  *                      a = gamma / sqrt(var + eps), S = sum gy (x - mu), M = N*H*W, mu and var recomputed
  *                      from x; gw (optional, fp32) receives C values dgamma = S / sqrt(var + eps), then
  *                      C values dbeta = sum gy.  Needs fwd.x resident; fwd.scale = gamma; gpre = gy.
+ *   DELTA_OP_LAYERNORM (bf16 and fp32) gx = (g - mean(g) - xh mean(g xh)) / sqrt(var + eps) (+ gx_add) per row, g = gy gamma, xh = (x - mean) /
+ *                      sqrt(var + eps), mean and var recomputed from x; gx_add is added before the one rounding.  gw (fp32) receives Cin values
+ *                      dgamma = sum gy xh, then Cin values dbeta = sum gy; needs a workspace.  gx or gw may be left out.  Needs fwd.x
+ *                      resident: the tensor, or (fwd.pack) its checkpoint; gx and gx_add have the bytes of the tensor; gpre = gy.
+ *   DELTA_OP_EMBEDDING (bf16 and fp32) gw[v][k] = scale_k * sum of gy[m,k] over the tokens m with id v: all rows of the fp32 table gradient are
+ *                      written, those of ids that do not occur with zeros; ids outside [0, Cin) count for nothing.  gw and a workspace
+ *                      are required, gx and gx_add must be unset; needs fwd.x (the ids) resident; gpre = gy.  Sums in a fixed order.
+ *   a linear layer     (DELTA_OP_CONV, 1x1, stride 1, bf16) with fwd.pack: as above, fwd.x being a checkpoint that the weight gradient reads;
+ *                      no mask_gx.
  *   DELTA_OP_RELU      (bf16) gx = gy * [y > 0] on the stored output; needs fwd.y resident; gpre = gy.
  *   the stem           (DELTA_OP_CONV, 7x7, stride 2, pad 3, 3 -> 64 channels, bf16): weight gradient only
  *                      (gw required, fp32 [64][7][7][3]; gx, gx_add must be unset); gpre (bytes of y) receives
@@ -359,9 +387,10 @@ typedef struct delta_bwd_desc {
                                   (a consumer ran with mask_gx): fwd.y is not read; with stride 1 gpre must
                                   be gy, with stride > 1 gpre receives gy spread to the input's resolution */
     const void *wt;            /* device: weights prepared by delta_bwd_weights (needed when gx is set) */
-    void *gw;                  /* device, fp32 [Cout][R][S][Cin]: receives dL/dw (overwritten), or NULL */
+    void *gw;                  /* device, fp32 [Cout][R][S][Cin] (other operators: above): receives dL/dw (overwritten), or NULL */
     void *workspace;           /* device scratch, 256-byte aligned: the weight gradient's partial sums (from
-                                  its start; at its end where both gradients are made in one pass) and,
+                                  its start; at its end where both gradients are made in one pass, and for layer
+                                  normalisation and the embedding) and,
                                   for a strided 1x1 layer, its staging tensor (at its end); needed when gw is
                                   set or (strided 1x1) gx is set.  A layer whose bytes at the end (staging, or
                                   the sums of one pass) overlap what weight gradients still in flight use makes
@@ -380,6 +409,9 @@ delta_status delta_bwd_weights(delta_ctx *ctx, const delta_layer_desc *layer, vo
 /* Bytes of workspace with which delta_backward_segment runs this layer as it does best (0 for operators that need none).
  * Not part of the arena: about 34 MB for 256 -> 128 or 512 -> 128 channels at 128 x 56 x 56 or 128 x 28 x 28. */
 delta_status delta_backward_workspace(delta_ctx *ctx, const delta_layer_desc *layer, uint64_t *out_bytes);
+/* Bytes of the checkpoint (DELTA_OP_PACK8) of a tensor of `rows` rows of `channels` channels, a multiple of 8.  Pure CPU: also on a
+ * planner-only context. */
+delta_status delta_packed_bytes(delta_ctx *ctx, uint64_t rows, uint32_t channels, uint64_t *out_bytes);
 /* Runs the descriptors in order on the compute stream.  Everything is validated before the first
  * launch.  Output tensors are allocated from the arena when not resident (DELTA_ERR_OOM_ARENA);
  * a non-resident input is DELTA_ERR_STATE.

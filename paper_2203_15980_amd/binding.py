@@ -18,6 +18,8 @@ NO_TENSOR = 0xFFFFFFFF
 WGRAD_S2_MAX_Q = 51     # output columns up to which a 3x3 stride-2 layer's weight gradient runs at the output's resolution
 OP_CONV, OP_MAXPOOL, OP_AVGPOOL, OP_SOFTMAX_CE, OP_ATTENTION, OP_LAYERNORM = 0, 1, 2, 3, 4, 5
 OP_BATCHNORM, OP_RELU, OP_ADD = 6, 7, 8
+OP_PACK8, OP_UNPACK8, OP_EMBEDDING = 9, 10, 11
+PACK_NONE, PACK_INT8, PACK_E4M3 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 FUSE_NONE, FUSE_BLOCK, FUSE_NO_STORE = 0, 1, 2
 
@@ -27,7 +29,7 @@ EXPORTS = ["delta_create", "delta_destroy", "delta_last_error", "delta_plan", "d
            "delta_stats_reset", "delta_set_skip_copies", "delta_probe_hostlink",
            "delta_probe_hbm", "delta_probe_mfma", "delta_layer_kernel", "delta_backward_kernel", "delta_bwd_weights",
            "delta_backward_workspace", "delta_backward_segment", "delta_backward_join",
-           "delta_batchnorm_static", "delta_reserve_pinned"]
+           "delta_batchnorm_static", "delta_reserve_pinned", "delta_packed_bytes"]
 
 
 class TensorDesc(C.Structure):
@@ -58,7 +60,7 @@ class LayerDesc(C.Structure):
                 ("N", C.c_int32), ("H", C.c_int32), ("W", C.c_int32), ("Cin", C.c_int32),
                 ("Cout", C.c_int32), ("R", C.c_int32), ("S", C.c_int32), ("stride", C.c_int32),
                 ("pad", C.c_int32), ("relu", C.c_uint32), ("op", C.c_uint32), ("eps", C.c_float),
-                ("fuse", C.c_uint32)]
+                ("fuse", C.c_uint32), ("pack", C.c_uint32)]
 
 
 class BwdDesc(C.Structure):
@@ -137,6 +139,7 @@ def load_library():
         "delta_backward_join": (i32, [vp]),
         "delta_batchnorm_static": (i32, [vp, vp, vp, vp, vp, u64, u32, C.c_float]),
         "delta_reserve_pinned": (i32, [vp, u64]),
+        "delta_packed_bytes": (i32, [vp, u64, u32, C.POINTER(u64)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -276,6 +279,12 @@ class Delta:
     def backward_workspace(self, layer):
         v = C.c_uint64()
         self._check(self.lib.delta_backward_workspace(self.ctx, layer_array([layer]), C.byref(v)))
+        return v.value
+
+    def packed_bytes(self, rows, channels):
+        """Bytes of the 8-bit checkpoint of a [rows, channels] tensor (OP_PACK8); also on a planner-only context."""
+        v = C.c_uint64()
+        self._check(self.lib.delta_packed_bytes(self.ctx, rows, channels, C.byref(v)))
         return v.value
 
     def backward_segment(self, descs):

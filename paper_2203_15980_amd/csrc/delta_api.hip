@@ -29,6 +29,7 @@
 
 #include "../../include/delta.h"
 #include "kernels.hpp"
+#include "packed.hpp"
 #include "planner.hpp"
 
 namespace {
@@ -761,9 +762,15 @@ delta_status delta_prefetch(delta_ctx *c, uint32_t id) {
     return DELTA_OK;
 }
 
-// Shape and size checks of one layer; fills the launch arguments except device addresses.
+// Bytes of the tensor that a layer reads, were it not a checkpoint: also those of its gradient.
+static uint64_t input_bytes(const delta_layer_desc &L) {
+    return (uint64_t)L.N * L.H * L.W * L.Cin * (L.dtype == DELTA_DTYPE_BF16 ? 2 : 4);
+}
+
+// Shape and size checks of one layer; fills the launch arguments except device addresses.  `backward`: the layer of a backward descriptor, whose x may
+// be a checkpoint where its operator reads one.
 static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint32_t i, delta::ConvArgs &a,
-                                  delta::PoolArgs &pa, uint64_t &flops) {
+                                  delta::PoolArgs &pa, uint64_t &flops, bool backward = false) {
     const size_t nt = c->tensors.size();
     if (L.x >= nt || L.y >= nt || (L.res != DELTA_NO_TENSOR && L.res >= nt))
         return fail(c, DELTA_ERR_INVALID, "layer %u: tensor id out of range", i);
@@ -774,7 +781,14 @@ static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint3
         return fail(c, DELTA_ERR_INVALID, "layer %u: non-positive dimension", i);
     const bool bf16 = L.dtype == DELTA_DTYPE_BF16;
     const uint64_t es = bf16 ? 2 : 4;
-    const uint64_t xbytes = (uint64_t)L.N * L.H * L.W * L.Cin * es;
+    const bool packs = L.op == DELTA_OP_PACK8 || L.op == DELTA_OP_UNPACK8;
+    if (L.pack > DELTA_PACK_E4M3 || (packs && !L.pack)) return fail(c, DELTA_ERR_INVALID, "layer %u: unknown checkpoint format %u", i, L.pack);
+    if (L.pack && !packs && !(backward && (L.op == DELTA_OP_LAYERNORM || L.op == DELTA_OP_CONV)))
+        return fail(c, DELTA_ERR_INVALID, "layer %u: a checkpoint is read by DELTA_OP_UNPACK8 and by the backward of layer normalisation and of linear "
+                    "layers only", i);
+    const long long rows = (long long)L.N * L.H * L.W;
+    const uint64_t plain = input_bytes(L), held = L.pack ? delta::packed_bytes((uint64_t)rows, (uint64_t)L.Cin) : 0;
+    const uint64_t xbytes = L.op == DELTA_OP_EMBEDDING ? (uint64_t)rows * 8 : L.pack && L.op != DELTA_OP_PACK8 ? held : plain;
     if (c->tensors[L.x].bytes != xbytes)
         return fail(c, DELTA_ERR_INVALID, "layer %u: input tensor %u has %llu bytes, layer needs %llu", i, L.x,
                     (unsigned long long)c->tensors[L.x].bytes, (unsigned long long)xbytes);
@@ -846,9 +860,25 @@ static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint3
         if (L.Cout != L.Cin) return fail(c, DELTA_ERR_INVALID, "layer %u: layer normalisation keeps the shape", i);
         if (L.res != DELTA_NO_TENSOR) return fail(c, DELTA_ERR_INVALID, "layer %u: layer normalisation takes no second input", i);
         if (!(L.eps >= 0.f)) return fail(c, DELTA_ERR_INVALID, "layer %u: eps must be >= 0", i);
-        const char *why = delta::layernorm_check(c->arena, c->arena, L.scale, L.shift, (long long)L.N * L.H * L.W, L.Cin, bf16);
+        const char *why = delta::layernorm_check(c->arena, c->arena, L.scale, L.shift, rows, L.Cin, bf16);
         if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
-        ybytes = xbytes;
+        ybytes = plain;
+        break;
+    }
+    case DELTA_OP_PACK8:
+    case DELTA_OP_UNPACK8: {
+        if (L.Cout != L.Cin) return fail(c, DELTA_ERR_INVALID, "layer %u: a checkpoint keeps the shape", i);
+        if (L.res != DELTA_NO_TENSOR) return fail(c, DELTA_ERR_INVALID, "layer %u: a checkpoint takes no second input", i);
+        const char *why = delta::pack8_check(c->arena, c->arena, rows, L.Cin, (int)L.pack);
+        if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
+        ybytes = L.op == DELTA_OP_PACK8 ? held : plain;
+        break;
+    }
+    case DELTA_OP_EMBEDDING: {
+        if (L.res != DELTA_NO_TENSOR) return fail(c, DELTA_ERR_INVALID, "layer %u: the embedding takes no second input", i);
+        const char *why = delta::embedding_check(L.w, L.scale, rows, L.Cin, L.Cout);
+        if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
+        ybytes = (uint64_t)rows * L.Cout * es;
         break;
     }
     case DELTA_OP_BATCHNORM:
@@ -1105,6 +1135,14 @@ delta_status delta_recompute_segment(delta_ctx *c, const delta_layer_desc *layer
                 HIP_TRY(c, delta::launch_add(xp, rp, yp, ty.bytes, 1, c->stream[S_COMPUTE]));
             }
             break;
+        case DELTA_OP_PACK8:
+        case DELTA_OP_UNPACK8:
+            HIP_TRY(c, delta::launch_pack8(xp, yp, rows, L.Cin, L.dtype == DELTA_DTYPE_BF16, (int)L.pack, L.op == DELTA_OP_PACK8,
+                                           c->stream[S_COMPUTE]));
+            break;
+        case DELTA_OP_EMBEDDING:
+            HIP_TRY(c, delta::launch_embedding(xp, L.w, L.scale, yp, rows, L.Cin, L.Cout, L.dtype == DELTA_DTYPE_BF16, c->stream[S_COMPUTE]));
+            break;
         case DELTA_OP_LAYERNORM:
             HIP_TRY(c, delta::launch_layernorm(xp, yp, L.scale, L.shift, (long long)L.N * L.H * L.W, L.Cin, L.eps,
                                                L.dtype == DELTA_DTYPE_BF16, c->stream[S_COMPUTE]));
@@ -1294,7 +1332,7 @@ delta_status need_identity_factors(delta_ctx *c) {
     return DELTA_OK;
 }
 
-enum BwdKind { BK_CONV, BK_DENSE, BK_MAXPOOL, BK_AVGPOOL, BK_LOSS, BK_STEM, BK_BATCHNORM, BK_RELU };
+enum BwdKind { BK_CONV, BK_DENSE, BK_MAXPOOL, BK_AVGPOOL, BK_LOSS, BK_STEM, BK_BATCHNORM, BK_RELU, BK_LAYERNORM, BK_EMBEDDING };
 
 bool is_stem(const delta_layer_desc &L) {
     return L.op == DELTA_OP_CONV && L.dtype == DELTA_DTYPE_BF16 && L.R == 7 && L.S == 7 && L.stride == 2 && L.pad == 3 &&
@@ -1309,6 +1347,8 @@ BwdKind bwd_kind(const delta_layer_desc &L) {
     if (L.op == DELTA_OP_SOFTMAX_CE) return BK_LOSS;
     if (L.op == DELTA_OP_BATCHNORM) return BK_BATCHNORM;
     if (L.op == DELTA_OP_RELU) return BK_RELU;
+    if (L.op == DELTA_OP_LAYERNORM) return BK_LAYERNORM;
+    if (L.op == DELTA_OP_EMBEDDING) return BK_EMBEDDING;
     if (is_stem(L)) return BK_STEM;
     if (L.H == 1 && L.W == 1 && L.R == 1 && L.S == 1 && L.stride == 1 && L.pad == 0 && L.Cout % 64 != 0) return BK_DENSE;
     return BK_CONV;
@@ -1332,6 +1372,40 @@ delta_status prepare_backward_stem(delta_ctx *c, const delta_bwd_desc &D, uint32
     if (own_mask ? (D.gpre == D.gy || D.gpre == L.y || D.gpre == L.x) : D.gpre != D.gy)
         return fail(c, DELTA_ERR_INVALID, "backward %u: gpre must be a separate tensor exactly when a ReLU mask is applied", i);
     if (!D.workspace || ((uintptr_t)D.workspace & 255) || D.workspace_bytes < delta::stem_wgrad_workspace_bytes(fa))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: workspace missing, not 256-byte aligned or too small", i);
+    return DELTA_OK;
+}
+
+// Layer normalisation and the embedding: bf16 and fp32, gradients of the input, of the weights or of both, and a workspace for the latter.
+uint64_t row_op_workspace_bytes(const delta_layer_desc &L) {
+    const long long rows = (long long)L.N * L.H * L.W;
+    const uint64_t need = L.op == DELTA_OP_LAYERNORM ? delta::layernorm_bwd_workspace_bytes(rows, L.Cin) : delta::embedding_bwd_workspace_bytes(rows, L.Cin, L.Cout);
+    return (need + 255) / 256 * 256;
+}
+delta_status prepare_backward_rows(delta_ctx *c, const delta_bwd_desc &D, uint32_t i) {
+    delta::ConvArgs a;
+    delta::PoolArgs pa;
+    uint64_t flops = 0;
+    const delta_layer_desc &L = D.fwd;
+    delta_status r = prepare_layer(c, L, i, a, pa, flops, true);
+    if (r != DELTA_OK) return r;
+    const size_t nt = c->tensors.size();
+    const bool norm = L.op == DELTA_OP_LAYERNORM;
+    if (D.mask_gx || D.gy_masked) return fail(c, DELTA_ERR_INVALID, "backward %u: this operator has no masks", i);
+    if (D.gy >= nt || c->tensors[D.gy].bytes != c->tensors[L.y].bytes || D.gpre != D.gy)
+        return fail(c, DELTA_ERR_INVALID, "backward %u: gy must have the bytes of y and gpre must be gy", i);
+    if (!norm && (D.gx != DELTA_NO_TENSOR || D.gx_add != DELTA_NO_TENSOR || !D.gw))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: the embedding has a weight gradient only (gx, gx_add unused)", i);
+    if (D.gx == DELTA_NO_TENSOR && (!D.gw || D.gx_add != DELTA_NO_TENSOR))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: nothing to compute, or gx_add without gx", i);
+    if (D.gx != DELTA_NO_TENSOR) {
+        if (D.gx >= nt || c->tensors[D.gx].bytes != input_bytes(L) || D.gx == L.x || D.gx == L.y || D.gx == D.gy)
+            return fail(c, DELTA_ERR_INVALID, "backward %u: gx must be another tensor with the bytes of the unpacked x", i);
+        if (D.gx_add != DELTA_NO_TENSOR && (D.gx_add >= nt || c->tensors[D.gx_add].bytes != input_bytes(L) || D.gx_add == D.gx))
+            return fail(c, DELTA_ERR_INVALID, "backward %u: gx_add must be another tensor with the bytes of gx", i);
+    }
+    if (D.gw && ((uintptr_t)D.gw & 15)) return fail(c, DELTA_ERR_INVALID, "backward %u: gw misaligned", i);
+    if (D.gw && (!D.workspace || ((uintptr_t)D.workspace & 255) || D.workspace_bytes < row_op_workspace_bytes(L)))
         return fail(c, DELTA_ERR_INVALID, "backward %u: workspace missing, not 256-byte aligned or too small", i);
     return DELTA_OK;
 }
@@ -1451,7 +1525,7 @@ int runs_beside(const delta_ctx *c, const delta_bwd_desc &D, bool aside) { retur
 // layer's own geometry, `fa` after as_stride_1, `da` the data gradient's convolution.
 enum OneLaunch { OL_NONE, OL_LAYER, OL_CLASS, OL_WEIGHT, OL_JOINT };
 OneLaunch one_launch(const delta_bwd_desc &D, const delta::ConvArgs &fo, const delta::ConvArgs &fa, const delta::ConvArgs &da) {
-    if (!D.gw || D.gx == DELTA_NO_TENSOR) return OL_NONE;
+    if (!D.gw || D.gx == DELTA_NO_TENSOR || D.fwd.pack) return OL_NONE;
     if (!class_dgrad(D)) {
         if (delta::small_backward_applies(&da, fa)) return OL_LAYER;
         return delta::joint1x1_applies(fa) && D.workspace_bytes >= delta::joint1x1_workspace_bytes(fa) ? OL_JOINT : OL_NONE;
@@ -1475,6 +1549,7 @@ bool masks_on_the_way(const delta_bwd_desc &D, const delta::ConvArgs &fa, const 
 }
 // `fa` after as_stride_1
 uint64_t backward_workspace_bytes(const delta_layer_desc &L, const delta::ConvArgs &fa) {
+    if (L.pack) return ((uint64_t)delta::wgrad1x1_packed_workspace_bytes(fa) + 255) / 256 * 256;
     uint64_t need = partials_bytes(fa) + staging_bytes(L, fa);
     if (L.stride == 2 && L.R == 3 && L.S == 3 && L.pad == 1) {          // whichever way the weight gradient goes
         delta::ConvArgs fo = fa;
@@ -1490,7 +1565,7 @@ delta_status prepare_backward(delta_ctx *c, const delta_bwd_desc &D, uint32_t i,
     delta::PoolArgs pa;
     uint64_t flops = 0;
     const delta_layer_desc &L = D.fwd;
-    delta_status r = prepare_layer(c, L, i, fa, pa, flops);
+    delta_status r = prepare_layer(c, L, i, fa, pa, flops, true);
     if (r != DELTA_OK) return r;
     if (L.op != DELTA_OP_CONV) return fail(c, DELTA_ERR_INVALID, "backward %u: operator %u has no backward here", i, L.op);
     if (delta::stem_applies(fa)) return fail(c, DELTA_ERR_INVALID, "backward %u: the stem convolution has no backward here", i);
@@ -1500,7 +1575,10 @@ delta_status prepare_backward(delta_ctx *c, const delta_bwd_desc &D, uint32_t i,
     if (L.stride > 1 && L.res != DELTA_NO_TENSOR)
         return fail(c, DELTA_ERR_INVALID, "backward %u: a strided layer with a residual has no backward here", i);
     const size_t nt = c->tensors.size();
-    const uint64_t ybytes = c->tensors[L.y].bytes, xbytes = c->tensors[L.x].bytes;
+    const uint64_t ybytes = c->tensors[L.y].bytes, xbytes = input_bytes(L);
+    if (L.pack && D.mask_gx) return fail(c, DELTA_ERR_INVALID, "backward %u: mask_gx reads x itself, not a checkpoint of it", i);
+    if (L.pack && (L.dtype != DELTA_DTYPE_BF16 || L.R != 1 || L.S != 1 || L.stride != 1 || L.pad != 0))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: a checkpoint is read by linear layers (1x1, stride 1) in bf16", i);
     // gpre lives at the input's resolution (for stride 1 that is y's), except for strided 1x1
     // layers, which are handled at the output's resolution
     const bool direct = strided_1x1(L);
@@ -1551,7 +1629,7 @@ delta_status prepare_backward(delta_ctx *c, const delta_bwd_desc &D, uint32_t i,
     // 1x1 layer at the output's)
     as_stride_1(L, fa);
     if (D.gw) {
-        const char *why = class_wgrad(D, fo) ? nullptr : delta::wgrad_check(fa);
+        const char *why = class_wgrad(D, fo) ? nullptr : L.pack ? delta::wgrad1x1_packed_check(fa) : delta::wgrad_check(fa);
         if (why) return fail(c, DELTA_ERR_INVALID, "backward %u: %s", i, why);
         if ((uintptr_t)D.gw & 15) return fail(c, DELTA_ERR_INVALID, "backward %u: gw misaligned", i);
     }
@@ -1622,13 +1700,24 @@ delta_status delta_backward_workspace(delta_ctx *c, const delta_layer_desc *laye
     delta::ConvArgs a;
     delta::PoolArgs pa;
     uint64_t flops = 0;
-    if ((r = prepare_layer(c, *layer, 0, a, pa, flops)) != DELTA_OK) return r;
+    if ((r = prepare_layer(c, *layer, 0, a, pa, flops, true)) != DELTA_OK) return r;
+    if (layer->op == DELTA_OP_LAYERNORM || layer->op == DELTA_OP_EMBEDDING) { *out_bytes = row_op_workspace_bytes(*layer); return DELTA_OK; }
     if (layer->op != DELTA_OP_CONV) { *out_bytes = 0; return DELTA_OK; }
     if (is_stem(*layer)) { *out_bytes = delta::stem_wgrad_workspace_bytes(a); return DELTA_OK; }
     as_stride_1(*layer, a);
     *out_bytes = backward_workspace_bytes(*layer, a);            // what is needed; what the one-pass kernel can use
+    if (layer->pack) return DELTA_OK;
     const uint64_t joint = ((uint64_t)delta::joint1x1_workspace_bytes(a) + 255) / 256 * 256;
     if (*out_bytes < joint) *out_bytes = joint;
+    return DELTA_OK;
+}
+
+delta_status delta_packed_bytes(delta_ctx *c, uint64_t rows, uint32_t channels, uint64_t *out_bytes) {
+    if (!c) return DELTA_ERR_INVALID;
+    if (!out_bytes) return fail(c, DELTA_ERR_INVALID, "null output argument");
+    if (rows == 0 || rows > 0x7FFFFFFFull || channels == 0 || channels % 8 || channels > 0x7FFFFFFFu)
+        return fail(c, DELTA_ERR_INVALID, "packed_bytes: 1 to 2147483647 rows, channels a multiple of 8");
+    *out_bytes = delta::packed_bytes(rows, channels);
     return DELTA_OK;
 }
 
@@ -1650,6 +1739,15 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
             if (D.fwd.relu && !D.gy_masked && !there(D.fwd.y))
                 return fail(c, DELTA_ERR_STATE, "backward %u: y tensor %u is not resident", i, D.fwd.y);
             will_exist[D.gpre] = 1;
+            continue;
+        }
+        if (kind == BK_LAYERNORM || kind == BK_EMBEDDING) {
+            if ((r = prepare_backward_rows(c, D, i)) != DELTA_OK) return r;
+            if (!there(D.gy)) return fail(c, DELTA_ERR_STATE, "backward %u: gy tensor %u is not resident", i, D.gy);
+            if (!there(D.fwd.x)) return fail(c, DELTA_ERR_STATE, "backward %u: x tensor %u is not resident", i, D.fwd.x);
+            if (D.gx_add != DELTA_NO_TENSOR && !there(D.gx_add))
+                return fail(c, DELTA_ERR_STATE, "backward %u: gx_add tensor %u is not resident", i, D.gx_add);
+            if (D.gx != DELTA_NO_TENSOR) will_exist[D.gx] = 1;
             continue;
         }
         if (kind != BK_CONV) {
@@ -1702,6 +1800,36 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
             HIP_TRY(c, delta::launch_stem_wgrad(fa, c->arena + c->tensors[D.gpre].offset, static_cast<float *>(D.gw),
                                                 D.workspace, D.workspace_bytes, s));
             c->st.recompute_flops += 2ull * (uint64_t)fa.M * 7 * 7 * 3 * 64;
+            c->st.recompute_launches += 1;
+            continue;
+        }
+        if (kind == BK_LAYERNORM || kind == BK_EMBEDDING) {
+            if ((r = prepare_backward_rows(c, D, i)) != DELTA_OK) return r;
+            Tensor &tx = c->tensors[L.x], &tgy = c->tensors[D.gy];
+            if ((r = compute_uses(c, tx)) != DELTA_OK) return r;
+            if ((r = compute_uses(c, tgy)) != DELTA_OK) return r;
+            const unsigned char *addp = nullptr;
+            if (D.gx_add != DELTA_NO_TENSOR) {
+                if ((r = compute_uses(c, c->tensors[D.gx_add])) != DELTA_OK) return r;
+                addp = c->arena + c->tensors[D.gx_add].offset;
+            }
+            unsigned char *gxp = nullptr;
+            if (D.gx != DELTA_NO_TENSOR) {
+                if ((r = compute_writes(c, c->tensors[D.gx])) != DELTA_OK) return r;
+                gxp = c->arena + c->tensors[D.gx].offset;
+            }
+            // its sums at the END of the workspace: weight gradients still running on the other stream use its beginning
+            const uint64_t need = D.gw ? row_op_workspace_bytes(L) : 0;
+            unsigned char *sums = D.gw ? static_cast<unsigned char *>(D.workspace) + ((D.workspace_bytes - need) & ~(uint64_t)255) : nullptr;
+            if (D.gw && aux_holds(c, sums, need) && (r = join_aux(c)) != DELTA_OK) return r;
+            const long long rows = (long long)L.N * L.H * L.W;
+            const int bf16 = L.dtype == DELTA_DTYPE_BF16;
+            if (kind == BK_LAYERNORM)
+                HIP_TRY(c, delta::launch_layernorm_bwd(c->arena + tx.offset, c->arena + tgy.offset, addp, gxp, L.scale, static_cast<float *>(D.gw), rows,
+                                                       L.Cin, L.eps, bf16, (int)L.pack, sums, need, s));
+            else
+                HIP_TRY(c, delta::launch_embedding_bwd(c->arena + tx.offset, c->arena + tgy.offset, L.scale, static_cast<float *>(D.gw), rows, L.Cin,
+                                                       L.Cout, bf16, sums, need, s));
             c->st.recompute_launches += 1;
             continue;
         }
@@ -1897,7 +2025,7 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
             // its own stream, and both tensors remember that reader.
             // A small one stays on the compute stream, after whatever still uses the workspace on the other.
             const bool by_class = class_wgrad(D, fo);
-            const uint64_t need = by_class ? delta::wgrad_s2_workspace_bytes(fo) : partials_bytes(fa);
+            const uint64_t need = by_class ? delta::wgrad_s2_workspace_bytes(fo) : L.pack ? backward_workspace_bytes(L, fa) : partials_bytes(fa);
             hipStream_t gs = s;
             if (aside) {
                 gs = c->stream[S_AUX];
@@ -1910,7 +2038,8 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
                 HIP_TRY(c, delta::launch_wgrad_s2(fo, c->arena + tgy.offset, static_cast<float *>(D.gw), D.workspace, need, gs));
                 c->st.recompute_flops += 2ull * (uint64_t)fo.M * 9 * fo.Cin * fo.Cout;
             } else {
-                HIP_TRY(c, delta::launch_wgrad(fa, gp, static_cast<float *>(D.gw), D.workspace, need, gs));
+                if (L.pack) HIP_TRY(c, delta::launch_wgrad1x1_packed(fa, (int)L.pack, gp, static_cast<float *>(D.gw), D.workspace, need, gs));
+                else HIP_TRY(c, delta::launch_wgrad(fa, gp, static_cast<float *>(D.gw), D.workspace, need, gs));
                 c->st.recompute_flops += 2ull * (uint64_t)fa.M * fa.R * fa.S * fa.Cin * fa.Cout;
             }
             if (aside) {
@@ -1961,7 +2090,10 @@ delta_status delta_layer_kernel(delta_ctx *c, const delta_layer_desc *layer, cha
              : waves == 4 ? "attention bf16 (128 queries x 4 waves, K/V in LDS)" : "attention bf16 (64 queries x 2 waves, K/V in LDS)";
         break;
     }
-    case DELTA_OP_LAYERNORM: name = "layernorm bf16"; break;
+    case DELTA_OP_LAYERNORM: name = layer->dtype == DELTA_DTYPE_BF16 ? "layernorm bf16" : "layernorm f32"; break;
+    case DELTA_OP_PACK8: name = layer->pack == DELTA_PACK_INT8 ? "pack8 int8" : "pack8 e4m3"; break;
+    case DELTA_OP_UNPACK8: name = layer->pack == DELTA_PACK_INT8 ? "unpack8 int8" : "unpack8 e4m3"; break;
+    case DELTA_OP_EMBEDDING: name = layer->dtype == DELTA_DTYPE_BF16 ? "embedding bf16" : "embedding f32"; break;
     case DELTA_OP_BATCHNORM: name = "batchnorm (batch statistics) bf16: stats + finalize + one pass (with an add and ReLU that follow)"; break;
     case DELTA_OP_RELU: name = "relu bf16"; break;
     case DELTA_OP_ADD: name = "add bf16"; break;
@@ -1983,6 +2115,12 @@ delta_status delta_backward_kernel(delta_ctx *c, const delta_bwd_desc *desc, cha
     if (kind == BK_STEM) {
         if ((r = prepare_backward_stem(c, D, 0, fa)) != DELTA_OK) return r;
         snprintf(out, (size_t)cap, "gw: stem_wgrad");
+        return DELTA_OK;
+    }
+    if (kind == BK_LAYERNORM || kind == BK_EMBEDDING) {
+        if ((r = prepare_backward_rows(c, D, 0)) != DELTA_OK) return r;
+        const char *from = L.pack == DELTA_PACK_INT8 ? " from int8" : L.pack == DELTA_PACK_E4M3 ? " from e4m3" : "";
+        snprintf(out, (size_t)cap, "%s%s%s", D.gx == DELTA_NO_TENSOR ? "gw: " : D.gw ? "gx, gw: " : "gx: ", kind == BK_LAYERNORM ? "layernorm" : "embedding", from);
         return DELTA_OK;
     }
     if (kind != BK_CONV) {
@@ -2028,7 +2166,8 @@ delta_status delta_backward_kernel(delta_ctx *c, const delta_bwd_desc *desc, cha
             snprintf(gw, sizeof gw, "; gw: %s%s", one == OL_JOINT ? "joint1x1 bf16" : delta::small_backward_name(fa),
                      one == OL_LAYER || one == OL_JOINT ? ", the same launch" : one == OL_CLASS ? ", the launch of one class" : ", compute stream");
         else
-            snprintf(gw, sizeof gw, "%sgw: %s%s", gx[0] ? "; " : "", class_wgrad(D, fo) ? "wgrad3x3 stride 2 bf16" : delta::wgrad_kernel_name(fa),
+            snprintf(gw, sizeof gw, "%sgw: %s%s", gx[0] ? "; " : "", class_wgrad(D, fo) ? "wgrad3x3 stride 2 bf16" : L.pack == DELTA_PACK_INT8 ? "wgrad1x1 from int8" :
+                     L.pack ? "wgrad1x1 from e4m3" : delta::wgrad_kernel_name(fa),
                      wgrad_aside(L, fa) ? ", second stream" : ", compute stream");
     }
     snprintf(out, (size_t)cap, "%s%s", gx, gw);

@@ -155,6 +155,25 @@ const char *layernorm_check(const void *x, const void *y, const float *gamma, co
                             int bf16);
 hipError_t launch_layernorm(const void *x, void *y, const float *gamma, const float *beta, long long rows, int C,
                             float eps, int bf16, hipStream_t stream);
+// layernorm.hip: the same in fp32 or over more than 2048 channels (launch_layernorm calls it), and the gradients, also from a checkpoint x (fmt)
+hipError_t launch_layernorm_more(const void *x, void *y, const float *gamma, const float *beta, long long rows, int C, float eps, int bf16,
+                                 hipStream_t stream);
+size_t layernorm_bwd_workspace_bytes(long long rows, int C);
+hipError_t launch_layernorm_bwd(const void *x, const void *gy, const void *add, void *gx, const float *gamma, float *gw, long long rows, int C, float eps,
+                                int bf16, int fmt, void *workspace, size_t workspace_bytes, hipStream_t stream);
+// pack8.hip: an activation into its 8-bit checkpoint and back
+const char *pack8_check(const void *x, const void *y, long long rows, int C, int fmt);
+hipError_t launch_pack8(const void *x, void *y, long long rows, int C, int bf16, int fmt, bool pack, hipStream_t stream);
+// wgrad1x1_packed.hip: weight gradient of a linear layer whose input is such a checkpoint
+const char *wgrad1x1_packed_check(const ConvArgs &a);
+size_t wgrad1x1_packed_workspace_bytes(const ConvArgs &a);
+hipError_t launch_wgrad1x1_packed(const ConvArgs &a, int fmt, const void *g, float *gw, void *workspace, size_t workspace_bytes, hipStream_t stream);
+// embedding.hip: lookup of scaled table rows and the table's gradient
+const char *embedding_check(const void *w, const float *scale, long long n, long long V, int C);
+hipError_t launch_embedding(const void *id, const void *w, const float *scale, void *y, long long n, int V, int C, int bf16, hipStream_t stream);
+size_t embedding_bwd_workspace_bytes(long long n, int V, int C);
+hipError_t launch_embedding_bwd(const void *id, const void *gy, const float *scale, float *gw, long long n, int V, int C, int bf16, void *workspace,
+                                size_t workspace_bytes, hipStream_t stream);
 // opgranular_ops.hip: training-mode batch normalisation over [M, C] (bf16), ReLU, residual add
 const char *bn_train_check(const void *x, const void *y, const float *gamma, const float *beta, long long M, int C,
                            int bf16);

@@ -86,17 +86,19 @@ __global__ __launch_bounds__(kRowsPerBlock * 64) void layernorm_kernel(const uns
 
 const char *layernorm_check(const void *x, const void *y, const float *gamma, const float *beta, long long rows, int C,
                             int bf16) {
-    if (!bf16) return "layer normalisation is bf16 only";
-    if (rows <= 0 || C <= 0 || C % 8 || C > tops::kRounds * 512) return "channels must be a multiple of 8, at most 2048";
+    (void)bf16;
+    if (rows <= 0 || C <= 0 || C % 8 || C > 8192 || (C > tops::kRounds * 512 && C % 64))
+        return "channels must be a multiple of 8 up to 2048, a multiple of 64 up to 8192";
     if (!x || !y || !gamma || !beta || (((uintptr_t)x | (uintptr_t)y | (uintptr_t)gamma | (uintptr_t)beta) & 15))
         return "pointers must be non-null and 16-byte aligned";
-    if ((rows + tops::kRowsPerBlock - 1) / tops::kRowsPerBlock > 0x7FFFFFFFLL) return "too many rows";
+    if (rows > 0x7FFFFFFFLL) return "too many rows";
     return nullptr;
 }
 
 hipError_t launch_layernorm(const void *x, void *y, const float *gamma, const float *beta, long long rows, int C,
                             float eps, int bf16, hipStream_t stream) {
     if (layernorm_check(x, y, gamma, beta, rows, C, bf16)) return hipErrorInvalidValue;
+    if (!bf16 || C > tops::kRounds * 512) return launch_layernorm_more(x, y, gamma, beta, rows, C, eps, bf16, stream);
     const unsigned blocks = (unsigned)((rows + tops::kRowsPerBlock - 1) / tops::kRowsPerBlock);
     tops::layernorm_kernel<<<dim3(blocks), dim3(tops::kRowsPerBlock * 64), 0, stream>>>(
         static_cast<const unsigned char *>(x), static_cast<unsigned char *>(y), gamma, beta, rows, C, eps);
