@@ -2,17 +2,18 @@
 //   y[m] = scale * w[id[m]],   gw[v] = scale * sum over the m with id[m] = v of gy[m]        (scale: a factor per channel)
 // An id outside [0, V) stands for no token: its row of y is zero and its row of gy counts for nothing.
 //
-// Lookup: bound by memory, one read of a table row and one write for each token.  A thread keeps its eight channels' factors and has kAhead rows in flight.
+// Lookup: bound by memory, one read of a table row and one write for each token.  A thread keeps its eight channels' factors and has kLookups rows in flight.
 //
-// Gradient: every row of gw is written once, by one place, from the tokens in sorted order; no atomics on values, so the sums' order is fixed by
-// the ids alone.  What bounds it is the write of gw (4 V C bytes) beside one read of gy.
-//   * sort: stable radix sort of (id, position), two digits of half the id's bits each; a workgroup takes kSortItems tokens, ranks them by ballots within a
-//     wavefront, and finds its bases from all workgroups' digit counts itself; the first pass leaves the second one's counts (integer atomics: exact).
-//     Up to kSmall tokens one workgroup sorts (id, position) pairs in LDS by comparing and exchanging.
-//   * bounds: first and last place of each id that occurs; beside that, in the same launch, the sums of every aligned window of sorted places
-//     that holds one id only (frequent ids have many), each by a workgroup of its own.
-//   * rows: a row of gw adds its places before the first whole window, the windows' sums, and its places behind the last, or is zeros.
-// The window has about sqrt(tokens) / 2 places, so that a row's chain, of places and of windows, stays short even if all tokens are the same.
+// Gradient: rows of gw from the tokens in sorted order; no atomics on values, so the sums' order is fixed by the ids alone.  What bounds it is the write
+// of gw (4 V C bytes) beside one read of gy.
+//   * sort, and zeros beside it: gw is filled with zeros by the launches that sort, whose few workgroups leave the memory idle; rows of ids that occur are
+//     written once more (never more than there are tokens).  Up to kOneGroup tokens one workgroup sorts (id, position) pairs in
+//     LDS; beyond, a stable radix sort of two digits over all workgroups: each ranks kSortItems tokens by ballots within a wavefront
+//     and finds its bases from all workgroups' digit counts itself.
+//   * sums: a workgroup owns a chunk of sorted places, whose rows of gy it fetches 16 (fp32: 8) at a time, and adds up run by run.  A run of one id
+//     that begins and ends in the chunk is a row of gw; what a chunk holds of a run that goes on beyond it becomes a partial sum: its first run in slot 0
+//     if it came in from the chunk before, its last in slot 1 if it began here.  However often an id occurs, a chain is a chunk long.
+//   * joins: the chunk in which a run of several chunks begins adds its slot 1 and the following chunks' slots 0 up to the run's end, a row of gw.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -24,9 +25,9 @@ namespace emb {
 
 using rows::f32x4;
 
-constexpr int kAhead = 4;
-constexpr uint32_t kSmall = 2048;                        // most tokens that one workgroup sorts
-constexpr uint32_t kSortItems = 1024;                    // of a workgroup in the radix sort: 4 wavefronts, 4 rounds of 64 each
+constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup, chunks of the joins
+constexpr uint32_t kOneGroup = 16384;                    // most tokens that one workgroup sorts: 16 to a thread (64-bit items: a quarter)
+constexpr uint32_t kSortItems = 1024;                    // of a workgroup in the sort over all: 4 wavefronts, 4 rounds of 64 each
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
 constexpr long long kMostTokens = 1 << 24;
 
@@ -61,10 +62,10 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
     float f[8];
     factors(a.scale, piece, f);
     const uint32_t step = gridDim.x * a.side;
-    for (uint32_t m0 = blockIdx.x * a.side + at; m0 < a.n; m0 += kAhead * step) {
-        rows::Eight<T> raw[kAhead];
+    for (uint32_t m0 = blockIdx.x * a.side + at; m0 < a.n; m0 += kLookups * step) {
+        rows::Eight<T> raw[kLookups];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kLookups; ++i) {
             const uint32_t m = m0 + i * step;
             raw[i].zero();
             if (m >= a.n) continue;
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
             if ((uint64_t)id < a.V) raw[i].load(a.w + ((uint64_t)id * a.C + piece * 8) * sizeof(T));
         }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kLookups; ++i) {
             const uint32_t m = m0 + i * step;
             if (m >= a.n) continue;
             float v[8];
@@ -87,30 +88,31 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
 // ---- gradient
 struct Plan {
     uint32_t n, V, C;
-    uint32_t bits1, bits2;                               // of the two digits; an id of no token sorts as V, behind all others
-    uint32_t blocks, window, windows;
-    uint64_t key1, pos1, key2, pos2, hist1, hist2, first, last, sums, bytes;       // workspace: byte offsets and size
+    uint32_t bits, bits1, bits2;                         // of a key and its two digits; an id of no token sorts as V, behind all others
+    uint32_t blocks, chunk, chunks;
+    uint64_t key1, pos1, key2, pos2, hist1, hist2, sums, bytes;                    // workspace: byte offsets and size
 };
+
+// Whether one workgroup sorts all tokens.
+inline bool one_group(uint32_t n, uint32_t bits) { return n <= (bits + 14 > 32 ? kOneGroup / 4 : kOneGroup); }
 
 Plan plan_for(long long n, int V, int C) {
     Plan p;
     p.n = (uint32_t)n; p.V = (uint32_t)V; p.C = (uint32_t)C;
-    uint32_t bits = 1;
-    while ((1u << bits) <= (uint32_t)V) ++bits;
-    p.bits1 = (bits + 1) / 2;
-    p.bits2 = bits - p.bits1;
+    p.bits = 1;
+    while ((1u << p.bits) <= (uint32_t)V) ++p.bits;
+    p.bits1 = (p.bits + 1) / 2;
+    p.bits2 = p.bits - p.bits1;
     p.blocks = (p.n + kSortItems - 1) / kSortItems;
-    p.window = 32;
-    while ((uint64_t)p.window * p.window * 4 < p.n) p.window *= 2;
-    p.windows = p.n / p.window;                          // whole ones
+    p.chunk = p.n <= 16384 ? 16 : 32;
+    p.chunks = (p.n + p.chunk - 1) / p.chunk;
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const bool small = p.n <= kSmall;
-    p.key1 = take(small ? 0 : 4ull * p.n); p.pos1 = take(small ? 0 : 4ull * p.n);
+    const bool one = one_group(p.n, p.bits);
+    p.key1 = take(one ? 0 : 4ull * p.n); p.pos1 = take(one ? 0 : 4ull * p.n);
     p.key2 = take(4ull * p.n); p.pos2 = take(4ull * p.n);
-    p.hist1 = take(small ? 0 : (4ull << p.bits1) * p.blocks); p.hist2 = take(small ? 0 : (4ull << p.bits2) * p.blocks);
-    p.first = take(4ull * p.V); p.last = take(4ull * p.V);
-    p.sums = take(4ull * p.windows * p.C);
+    p.hist1 = take(one ? 0 : (4ull << p.bits1) * p.blocks); p.hist2 = take(one ? 0 : (4ull << p.bits2) * p.blocks);
+    p.sums = take(8ull * p.chunks * p.C);
     p.bytes = at;
     return p;
 }
@@ -120,67 +122,141 @@ struct Args {
     const unsigned char *gy;
     const float *scale;
     float *gw;
-    uint32_t *key1, *pos1, *key2, *pos2, *hist1, *hist2, *first, *last;
-    float *sums;
-    uint32_t n, V, C, bits1, bits2, blocks, window, windows, pieces, side;
+    uint32_t *key1, *pos1, *key2, *pos2, *hist1, *hist2;
+    float *sums;                                         // [chunks][2][C]
+    uint32_t n, V, C, bits, bits1, bits2, blocks, chunk, chunks, pieces;
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t id, uint32_t V) { return (uint64_t)id < V ? (uint32_t)id : V; }
 
-// Workgroups [from, gridDim.x) write zeros over `count` values.
-__device__ __forceinline__ void clear(uint32_t *p, uint64_t count, uint32_t from) {
-    for (uint64_t i = (uint64_t)(blockIdx.x - from) * blockDim.x + threadIdx.x; i < count; i += (uint64_t)(gridDim.x - from) * blockDim.x) p[i] = 0;
+// Part `part` of `parts` of gw filled with zeros by the workgroups from `from` on.
+__device__ __forceinline__ void fill(const Args &a, uint32_t from, uint32_t part, uint32_t parts) {
+    const uint64_t pieces = (uint64_t)a.V * a.C / 4, lo = pieces / parts * part, hi = part + 1 == parts ? pieces : pieces / parts * (part + 1);
+    f32x4 *p = reinterpret_cast<f32x4 *>(a.gw);
+    for (uint64_t i = lo + (uint64_t)(blockIdx.x - from) * blockDim.x + threadIdx.x; i < hi; i += (uint64_t)(gridDim.x - from) * blockDim.x)
+        p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// Workgroup 0 sorts all tokens; the others clear first and last.
-__global__ __launch_bounds__(1024) void sort_small_kernel(Args a) {
+// Ranks of 64 tokens by a digit d of `bits` bits: the lanes that hold the same digit (of those that are live), and how many of them come before this one.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, uint32_t bits, bool live) {
+    uint64_t same = __ballot(live);
+    for (uint32_t b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((d >> b) & 1);
+        same &= (d >> b) & 1 ? set : ~set;
+    }
+    return same;
+}
+
+// Workgroup 0 sorts all tokens; the others fill gw.  T: (id, position) in 32 or 64 bits, the position in the low 14.  A thread holds ITEMS neighbouring
+// items; a pass (at most 5 bits) counts each thread's digits in a column of its own, sums the counts by (digit, thread), which is the sorted order of
+// equal digits, and moves each item to its count's sum.  Every 16th word of LDS is followed by an unused one: a thread's words lie side by side.
+template <typename T, int ITEMS, int THREADS>
+struct SortLds {
+    T item[ITEMS * THREADS * 17 / 16];
+    uint32_t count[THREADS * 16 * 17 / 16];              // two counts to a word, [digit][thread]
+    uint32_t part[THREADS / 64];
+};
+__device__ __forceinline__ uint32_t spaced(uint32_t i) { return i + (i >> 4); }
+
+template <typename T, int ITEMS, int THREADS>
+__global__ __launch_bounds__(THREADS) void sort_kernel(Args a) {
     if (blockIdx.x) {
-        clear(a.first, a.V, 1);
-        clear(a.last, a.V, 1);
+        fill(a, 1, 0, 1);
         return;
     }
-    __shared__ uint64_t item[kSmall];
-    uint32_t size = 64;
-    while (size < a.n) size *= 2;
-    for (uint32_t i = threadIdx.x; i < size; i += 1024) item[i] = i < a.n ? (uint64_t)key_of(a.id[i], a.V) << 32 | i : ~0ull;
-    __syncthreads();
-    for (uint32_t run = 2; run <= size; run *= 2)        // bitonic: all items are different, so any sort is a stable one
-        for (uint32_t d = run / 2; d; d /= 2) {
-            for (uint32_t t = threadIdx.x; t < size / 2; t += 1024) {
-                const uint32_t i = (t / d) * 2 * d + t % d, j = i + d;
-                const uint64_t x = item[i], y = item[j];
-                if ((x > y) == ((i & run) == 0)) { item[i] = y; item[j] = x; }
-            }
-            __syncthreads();
+    extern __shared__ __align__(16) unsigned char smem[];
+    SortLds<T, ITEMS, THREADS> &l = *reinterpret_cast<SortLds<T, ITEMS, THREADS> *>(smem);
+    uint16_t *const count = reinterpret_cast<uint16_t *>(l.count);
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    T item[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const uint32_t i = tid + k * THREADS;
+        item[k] = i < a.n ? (T)key_of(a.id[i], a.V) << 14 | i : ~(T)0;    // what is behind the last token sorts behind it: all its bits are set
+    }
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) l.item[spaced(tid + k * THREADS)] = item[k];
+    const uint32_t passes = (a.bits + 4) / 5, width = (a.bits + passes - 1) / passes, words = (1u << width) / 2;     // words of counts a thread sums
+    const uint32_t column = spaced(tid / 2) * 2 + (tid & 1);
+    auto at = [&](uint32_t d) { return d * (THREADS * 17 / 16) + column; };         // spaced(d * THREADS / 2 + tid / 2): THREADS / 2 is a multiple of 16
+    for (uint32_t p = 0; p < passes; ++p) {
+        const uint32_t shift = 14 + p * width, mask = (1u << width) - 1;
+        for (uint32_t i = tid; i < spaced(words * THREADS); i += THREADS) l.count[i] = 0;
+        __syncthreads();
+        uint32_t rank[ITEMS];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) item[k] = l.item[spaced(tid * ITEMS + k)];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const uint32_t i = at((uint32_t)(item[k] >> shift) & mask);
+            rank[k] = count[i];
+            count[i] = (uint16_t)(rank[k] + 1);
         }
-    for (uint32_t i = threadIdx.x; i < a.n; i += 1024) {
-        a.key2[i] = (uint32_t)(item[i] >> 32);
-        a.pos2[i] = (uint32_t)item[i];
+        __syncthreads();
+        uint32_t w[16], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            w[j] = (uint32_t)j < words ? l.count[spaced(tid * words + j)] : 0;
+            sum += (w[j] & 0xFFFFu) + (w[j] >> 16);
+        }
+        uint32_t run = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const uint32_t v = __shfl_up(run, o, 64);
+            if ((int)lane >= o) run += v;
+        }
+        if (lane == 63) l.part[wave] = run;
+        __syncthreads();
+        run -= sum;
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) run += (uint32_t)i < wave ? l.part[i] : 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if ((uint32_t)j >= words) break;
+            const uint32_t second = run + (w[j] & 0xFFFFu);
+            l.count[spaced(tid * words + j)] = run | second << 16;
+            run = second + (w[j] >> 16);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) l.item[spaced(count[at((uint32_t)(item[k] >> shift) & mask)] + rank[k])] = item[k];
+        __syncthreads();
+    }
+    for (uint32_t i = tid; i < a.n; i += THREADS) {
+        const T v = l.item[spaced(i)];
+        a.key2[i] = (uint32_t)(v >> 14);
+        a.pos2[i] = (uint32_t)v & 16383u;
     }
 }
 
-// Digit counts of the first pass, [block][digit]; the workgroups behind clear the second pass's counts, first and last.
+// Digit counts of a pass, [block][digit]; the workgroups behind fill gw.
+template <bool FIRST>
 __global__ __launch_bounds__(256) void count_kernel(Args a) {
     if (blockIdx.x >= a.blocks) {
-        clear(a.hist2, (uint64_t)a.blocks << a.bits2, a.blocks);
-        clear(a.first, a.V, a.blocks);
-        clear(a.last, a.V, a.blocks);
+        fill(a, a.blocks, FIRST ? 0 : 2, 4);
         return;
     }
     __shared__ uint32_t bins[kMostBins];
-    const uint32_t nbins = 1u << a.bits1;
+    const uint32_t nbins = 1u << (FIRST ? a.bits1 : a.bits2), i0 = blockIdx.x * kSortItems;
+    uint32_t *hist = (FIRST ? a.hist1 : a.hist2) + (uint64_t)blockIdx.x * nbins;
     for (uint32_t i = threadIdx.x; i < nbins; i += 256) bins[i] = 0;
     __syncthreads();
-    const uint32_t i0 = blockIdx.x * kSortItems;
-    for (uint32_t i = threadIdx.x; i < kSortItems; i += 256)
-        if (i0 + i < a.n) atomicAdd(&bins[key_of(a.id[i0 + i], a.V) & (nbins - 1)], 1u);
+#pragma unroll
+    for (uint32_t r = 0; r < kSortItems / 256; ++r) {
+        const uint32_t i = i0 + r * 256 + threadIdx.x;
+        if (i < a.n) atomicAdd(&bins[FIRST ? key_of(a.id[i], a.V) & (nbins - 1) : a.key1[i] >> a.bits1], 1u);
+    }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < nbins; i += 256) a.hist1[(uint64_t)blockIdx.x * nbins + i] = bins[i];
+    for (uint32_t i = threadIdx.x; i < nbins; i += 256) hist[i] = bins[i];
 }
 
 // One pass of the sort: each token to its place by the digit, in the order the tokens come in.
 template <bool FIRST>
 __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
+    if (blockIdx.x >= a.blocks) {
+        fill(a, a.blocks, FIRST ? 1 : 3, 4);
+        return;
+    }
     __shared__ uint32_t base[kMostBins];                 // where this workgroup's tokens of a digit begin
     __shared__ uint32_t mine[4][kMostBins];              // tokens of a digit in each wavefront; then in those before it
     __shared__ uint32_t part[256];
@@ -199,6 +275,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
         const uint32_t d = tid * per + k;
         all[k] = 0;
         if ((uint32_t)k >= per || d >= nbins) continue;
+#pragma unroll 8
         for (uint32_t b = 0; b < a.blocks; ++b) {
             const uint32_t c = hist[(uint64_t)b * nbins + d];
             before[k] += b < blockIdx.x ? c : 0;
@@ -235,11 +312,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
             if (!FIRST) pos[r] = a.pos1[i];
         }
         const uint32_t d = (key[r] >> shift) & (nbins - 1);
-        uint64_t same = __ballot(live);
-        for (uint32_t b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot((d >> b) & 1);
-            same &= (d >> b) & 1 ? set : ~set;
-        }
+        const uint64_t same = same_digit(d, bits, live);
         const uint32_t lower = (uint32_t)__popcll(same & ((1ull << lane) - 1));
         volatile uint32_t *count = &mine[wave][d];
         const uint32_t had = live ? *count : 0;
@@ -266,7 +339,6 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
         if (FIRST) {
             a.key1[to] = key[r];
             a.pos1[to] = pos[r];
-            atomicAdd(&a.hist2[((uint64_t)(to / kSortItems) << a.bits2) + (key[r] >> a.bits1)], 1u);
         } else {
             a.key2[to] = key[r];
             a.pos2[to] = pos[r];
@@ -274,77 +346,113 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     }
 }
 
-// sum += rows [from, to) of gy in sorted order, kAhead rows in flight
-template <typename T>
-__device__ __forceinline__ void add_places(const Args &a, uint32_t from, uint32_t to, uint32_t piece, float (&sum)[8]) {
-    for (uint32_t i = from; i < to; i += kAhead) {
-        rows::Eight<T> raw[kAhead];
+__device__ __forceinline__ void put(float *out, const float (&v)[8]) {
+    reinterpret_cast<f32x4 *>(out)[0] = f32x4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<f32x4 *>(out)[1] = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+// A workgroup's chunk of sorted places, run by run, PLACES rows in flight.
+template <typename T, int PLACES>
+__global__ __launch_bounds__(1024) void sums_kernel(Args a) {
+    const uint32_t piece = threadIdx.x, lane = piece & 63, from = blockIdx.x * a.chunk, size = from + a.chunk < a.n ? a.chunk : a.n - from;
+    const uint32_t mine = from + (lane < size ? lane : size - 1);                  // a lane to a place: chunks have at most 64
+    const uint32_t keys = a.key2[mine], places = a.pos2[mine];
+    const uint32_t before = from ? a.key2[from - 1] : ~0u, after = from + size < a.n ? a.key2[from + size] : ~0u;
+    const bool live = piece < a.pieces;                  // the last wavefront's spare lanes only lend their place
+    float f[8], sum[8];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+    for (int e = 0; e < 8; ++e) f[e] = sum[e] = 0.f;
+    if (live) factors(a.scale, piece, f);
+    uint32_t run = (uint32_t)__builtin_amdgcn_readlane((int)keys, 0);              // the run that is being added up
+    bool came = run == before;                           // whether it came in from the chunk before
+    auto close = [&](bool goes_on) {
+        if (run >= a.V || !live) return;
+        if (came || goes_on) {
+            put(a.sums + ((uint64_t)blockIdx.x * 2 + (came ? 0 : 1)) * a.C + piece * 8, sum);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] *= f[e];
+            put(a.gw + (uint64_t)run * a.C + piece * 8, sum);
+        }
+    };
+    for (uint32_t i = 0; i < size; i += PLACES) {
+        rows::Eight<T> raw[PLACES];
+#pragma unroll
+        for (int k = 0; k < PLACES; ++k) {
+            const uint32_t m = (uint32_t)__builtin_amdgcn_readlane((int)places, (int)(i + k));         // behind the chunk: its last place
             raw[k].zero();
-            if (i + k < to) raw[k].load(a.gy + ((uint64_t)a.pos2[i + k] * a.C + piece * 8) * sizeof(T));
+            if (live && (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)(i + k)) < a.V) raw[k].load(a.gy + (uint64_t)m * a.C * sizeof(T) + piece * 8 * sizeof(T));
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < PLACES; ++k) {
+            if (i + k >= size) break;
+            const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)(i + k));
+            if (key != run) {
+                close(false);
+                run = key;
+                came = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+            }
             float v[8];
             raw[k].to(v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += v[e];
         }
     }
+    close(run == after);
 }
 
-// Workgroups [0, windows): the sum of a window that holds one id; the others: where each id begins and ends.
-template <typename T>
-__global__ __launch_bounds__(1024) void bounds_kernel(Args a) {
-    if (blockIdx.x >= a.windows) {
-        const uint32_t i = (blockIdx.x - a.windows) * blockDim.x + threadIdx.x;
-        if (i >= a.n) return;
-        const uint32_t k = a.key2[i];
-        if (k >= a.V) return;
-        if (i == 0 || a.key2[i - 1] != k) a.first[k] = i;
-        if (i + 1 == a.n || a.key2[i + 1] != k) a.last[k] = i + 1;
-        return;
-    }
-    const uint32_t from = blockIdx.x * a.window, k = a.key2[from];
-    if (k >= a.V || a.key2[from + a.window - 1] != k || threadIdx.x >= a.pieces) return;
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    add_places<T>(a, from, from + a.window, threadIdx.x, sum);
-    float *out = a.sums + (uint64_t)blockIdx.x * a.C + threadIdx.x * 8;
-    reinterpret_cast<f32x4 *>(out)[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
-    reinterpret_cast<f32x4 *>(out)[1] = f32x4{sum[4], sum[5], sum[6], sum[7]};
-}
-
-template <typename T>
-__global__ __launch_bounds__(1024) void rows_kernel(Args a) {
-    const uint32_t piece = threadIdx.x % a.pieces, at = threadIdx.x / a.pieces;
-    if (at >= a.side) return;
-    const uint32_t v = blockIdx.x * a.side + at;
-    if (v >= a.V) return;
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const uint32_t from = a.first[v], to = a.last[v];
-    if (from < to) {
-        const uint32_t lo = (from + a.window - 1) / a.window, hi = to / a.window;      // whole windows [lo, hi)
-        if (lo < hi) {
-            add_places<T>(a, from, lo * a.window, piece, sum);
-            for (uint32_t j = lo; j < hi; ++j) {
-                const f32x4 *p = reinterpret_cast<const f32x4 *>(a.sums + (uint64_t)j * a.C + piece * 8);
-                const f32x4 x = p[0], y = p[1];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { sum[e] += x[e]; sum[4 + e] += y[e]; }
-            }
-            add_places<T>(a, hi * a.window, to, piece, sum);
-        } else {
-            add_places<T>(a, from, to, piece, sum);
+// The runs that begin in this workgroup's chunk and go on into the next: slot 1 of this chunk, then slots 0 of the following ones that begin with the same id.
+// Threads: `side` groups of `pieces`; group g adds every side-th of those chunks, and the groups' sums are added in their order.
+__global__ __launch_bounds__(1024) void joins_kernel(Args a, uint32_t side) {
+    extern __shared__ __align__(16) float part[];        // [side][C]
+    const uint32_t next = (blockIdx.x + 1) * a.chunk, key = a.key2[next];          // one workgroup fewer than there are chunks
+    if (key >= a.V || a.key2[next - 1] != key) return;
+    if (blockIdx.x && a.key2[next - a.chunk] == key && a.key2[next - a.chunk - 1] == key) return;      // it began further back
+    uint32_t following = 0;                              // chunks that begin with this id, 64 looked at together
+    for (;;) {
+        const uint64_t at = (uint64_t)(blockIdx.x + 1 + following + (threadIdx.x & 63)) * a.chunk;
+        const uint64_t others = __ballot(at >= a.n || a.key2[at] != key);
+        if (others) {
+            following += (uint32_t)__builtin_ctzll(others);
+            break;
         }
-        float f[8];
-        factors(a.scale, piece, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] *= f[e];
+        following += 64;
     }
-    float *out = a.gw + (uint64_t)v * a.C + piece * 8;
-    reinterpret_cast<f32x4 *>(out)[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
-    reinterpret_cast<f32x4 *>(out)[1] = f32x4{sum[4], sum[5], sum[6], sum[7]};
+    const uint32_t piece = threadIdx.x % a.pieces, group = threadIdx.x / a.pieces;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (group < side) {
+        // place 0 is this chunk's slot 1, place j the j-th following chunk's slot 0
+        const uint32_t places = following + 1;
+        for (uint32_t j0 = group; j0 < places; j0 += side * kAhead) {
+            f32x4 v[kAhead][2];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const uint32_t j = j0 + k * side;
+                v[k][0] = v[k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (j >= places) continue;
+                const f32x4 *at = reinterpret_cast<const f32x4 *>(a.sums + ((uint64_t)(blockIdx.x + j) * 2 + (j ? 0 : 1)) * a.C + piece * 8);
+                v[k][0] = at[0];
+                v[k][1] = at[1];
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { sum[e] += v[k][0][e]; sum[4 + e] += v[k][1][e]; }
+        }
+        put(part + (uint64_t)group * a.C + piece * 8, sum);
+    }
+    __syncthreads();
+    if (group) return;
+    for (uint32_t g = 1; g < side; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += part[g * a.C + piece * 8 + e];
+    float f[8];
+    factors(a.scale, piece, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] *= f[e];
+    put(a.gw + (uint64_t)key * a.C + piece * 8, sum);
 }
 
 }  // namespace emb
@@ -364,7 +472,7 @@ hipError_t launch_embedding(const void *id, const void *w, const float *scale, v
     a.id = static_cast<const int64_t *>(id); a.w = static_cast<const unsigned char *>(w); a.y = static_cast<unsigned char *>(y); a.scale = scale;
     a.n = (uint32_t)n; a.V = (uint32_t)V; a.C = (uint32_t)C; a.pieces = r.pieces; a.side = r.side;
     const long long want = (n + r.side - 1) / r.side;
-    const dim3 grid((unsigned)(want < 2048 ? want : 2048)), block(r.threads);
+    const dim3 grid((unsigned)(want < 4096 ? want : 4096)), block(r.threads);
     if (bf16) emb::lookup_kernel<rows::bf16><<<grid, block, 0, stream>>>(a);
     else emb::lookup_kernel<float><<<grid, block, 0, stream>>>(a);
     return hipGetLastError();
@@ -372,20 +480,44 @@ hipError_t launch_embedding(const void *id, const void *w, const float *scale, v
 
 size_t embedding_bwd_workspace_bytes(long long n, int V, int C) { return emb::plan_for(n, V, C).bytes; }
 
+// Workgroups that fill gw beside a sort: enough to keep the memory busy, no more than there is work for.
+static uint32_t fillers(const emb::Args &a, uint32_t threads, uint32_t parts) {
+    const uint64_t want = (uint64_t)a.V * a.C / 4 / parts / (threads * 4) + 1, most = 2048 * 256 / threads;
+    return (uint32_t)(want < most ? want : most);
+}
+
+template <typename T, int ITEMS, int THREADS>
+static hipError_t embedding_sort(const emb::Args &a, hipStream_t stream) {
+    const int lds = (int)sizeof(emb::SortLds<T, ITEMS, THREADS>);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&emb::sort_kernel<T, ITEMS, THREADS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    emb::sort_kernel<T, ITEMS, THREADS><<<dim3(1 + fillers(a, THREADS, 1)), dim3(THREADS), lds, stream>>>(a);
+    return hipGetLastError();
+}
+
 template <typename T>
-static hipError_t embedding_bwd(const emb::Args &a, const emb::Rows &r, hipStream_t stream) {
+static hipError_t embedding_bwd(const emb::Args &a, hipStream_t stream) {
     using namespace emb;
-    const uint32_t clearing = a.V / 4096 + 1;
-    if (a.n <= kSmall) {
-        sort_small_kernel<<<dim3(1 + clearing), dim3(1024), 0, stream>>>(a);
+    if (one_group(a.n, a.bits)) {
+        const bool wide = a.bits + 14 > 32;
+        hipError_t e;
+        if (a.n <= 1024) e = wide ? embedding_sort<uint64_t, 4, 256>(a, stream) : embedding_sort<uint32_t, 4, 256>(a, stream);
+        else if (a.n <= 4096) e = wide ? embedding_sort<uint64_t, 4, 1024>(a, stream) : embedding_sort<uint32_t, 4, 1024>(a, stream);
+        else e = embedding_sort<uint32_t, 16, 1024>(a, stream);
+        if (e != hipSuccess) return e;
     } else {
-        count_kernel<<<dim3(a.blocks + clearing), dim3(256), 0, stream>>>(a);
-        scatter_kernel<true><<<dim3(a.blocks), dim3(256), 0, stream>>>(a);
-        scatter_kernel<false><<<dim3(a.blocks), dim3(256), 0, stream>>>(a);
+        const dim3 grid(a.blocks + fillers(a, 256, 4)), block(256);
+        count_kernel<true><<<grid, block, 0, stream>>>(a);
+        scatter_kernel<true><<<grid, block, 0, stream>>>(a);
+        count_kernel<false><<<grid, block, 0, stream>>>(a);
+        scatter_kernel<false><<<grid, block, 0, stream>>>(a);
     }
     const uint32_t threads = (a.pieces + 63) / 64 * 64;
-    bounds_kernel<T><<<dim3(a.windows + (a.n + threads - 1) / threads), dim3(threads), 0, stream>>>(a);
-    rows_kernel<T><<<dim3((a.V + a.side - 1) / a.side), dim3(r.threads), 0, stream>>>(a);
+    sums_kernel<T, sizeof(T) == 2 ? 16 : 8><<<dim3(a.chunks), dim3(threads), 0, stream>>>(a);
+    if (a.chunks > 1) {
+        const uint32_t side = a.pieces >= 256 ? 1 : 512 / a.pieces < 8 ? 512 / a.pieces : 8;
+        joins_kernel<<<dim3(a.chunks - 1), dim3((a.pieces * side + 63) / 64 * 64), side * a.C * sizeof(float), stream>>>(a, side);
+    }
     return hipGetLastError();
 }
 
@@ -395,17 +527,16 @@ hipError_t launch_embedding_bwd(const void *id, const void *gy, const float *sca
     if (embedding_check(gy, scale, n, V, C) || !id || !gw || !workspace || ((uintptr_t)workspace & 15)) return hipErrorInvalidValue;
     const emb::Plan p = emb::plan_for(n, V, C);
     if (workspace_bytes < p.bytes) return hipErrorInvalidValue;
-    const emb::Rows r = emb::rows_of(C);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     auto u32 = [&](uint64_t o) { return reinterpret_cast<uint32_t *>(ws + o); };
     emb::Args a;
     a.id = static_cast<const int64_t *>(id); a.gy = static_cast<const unsigned char *>(gy); a.scale = scale; a.gw = gw;
     a.key1 = u32(p.key1); a.pos1 = u32(p.pos1); a.key2 = u32(p.key2); a.pos2 = u32(p.pos2);
-    a.hist1 = u32(p.hist1); a.hist2 = u32(p.hist2); a.first = u32(p.first); a.last = u32(p.last);
+    a.hist1 = u32(p.hist1); a.hist2 = u32(p.hist2);
     a.sums = reinterpret_cast<float *>(ws + p.sums);
-    a.n = p.n; a.V = p.V; a.C = p.C; a.bits1 = p.bits1; a.bits2 = p.bits2; a.blocks = p.blocks;
-    a.window = p.window; a.windows = p.windows; a.pieces = r.pieces; a.side = r.side;
-    return bf16 ? embedding_bwd<rows::bf16>(a, r, stream) : embedding_bwd<float>(a, r, stream);
+    a.n = p.n; a.V = p.V; a.C = p.C; a.bits = p.bits; a.bits1 = p.bits1; a.bits2 = p.bits2; a.blocks = p.blocks;
+    a.chunk = p.chunk; a.chunks = p.chunks; a.pieces = (uint32_t)C / 8;
+    return bf16 ? embedding_bwd<rows::bf16>(a, stream) : embedding_bwd<float>(a, stream);
 }
 
 }  // namespace delta
