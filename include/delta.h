@@ -416,7 +416,7 @@ delta_status delta_packed_bytes(delta_ctx *ctx, uint64_t rows, uint32_t channels
  * launch.  Output tensors are allocated from the arena when not resident (DELTA_ERR_OOM_ARENA);
  * a non-resident input is DELTA_ERR_STATE.
  * Weight gradients of convolutions (gw) of 1 GFLOP and more are the exception to "on the compute
- * stream", unless they are made in the data gradient's own launch (delta_backward_kernel says which): nothing later in the
+ * stream", unless they are made in the data gradient's own launch, or from a checkpoint without gx (delta_backward_kernel says which): nothing later in the
  * backward pass reads them, so they run on a stream of the library's own, beside the
  * data-gradient chain, each after the launches that produce its inputs.  The arena accounts for
  * these readers when a tensor is released or rewritten.  The gw buffers and the workspace are the

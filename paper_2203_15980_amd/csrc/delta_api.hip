@@ -1515,6 +1515,11 @@ bool wgrad_aside(const delta_layer_desc &L, const delta::ConvArgs &fa) {
     const uint64_t rows = L.stride == 2 && L.R == 3 ? (uint64_t)fa.M / 4 : (uint64_t)fa.M;
     return 2ull * rows * fa.R * fa.S * fa.Cin * fa.Cout >= kAsideFlops;
 }
+// From a checkpoint and without a data gradient beside it the weight gradient stays on the compute stream at any size: 768 -> 768 on 16384 tokens 48 us, 62 with
+// the events of the other stream.
+bool goes_aside(const delta_bwd_desc &D, const delta::ConvArgs &fa) {
+    return wgrad_aside(D.fwd, fa) && !(D.fwd.pack && D.gx == DELTA_NO_TENSOR);
+}
 // Whether a data gradient's launch has company: its layer's weight gradient or an earlier one's on the other stream.  With a mask it is taken to have, as
 // inside a network, where the layers before have left theirs.
 int runs_beside(const delta_ctx *c, const delta_bwd_desc &D, bool aside) { return D.mask_gx || aside || c->aux_tail; }
@@ -1945,7 +1950,7 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
         }
         const unsigned char *gp = c->arena + c->tensors[D.gpre].offset;
         Ev ready;
-        const bool aside = D.gw && one == OL_NONE && wgrad_aside(L, fa);
+        const bool aside = D.gw && one == OL_NONE && goes_aside(D, fa);
         if (D.gw) {
             if ((r = compute_uses(c, c->tensors[L.x])) != DELTA_OK) return r;
             fa.x = fo.x = c->arena + c->tensors[L.x].offset;
@@ -2168,7 +2173,7 @@ delta_status delta_backward_kernel(delta_ctx *c, const delta_bwd_desc *desc, cha
         else
             snprintf(gw, sizeof gw, "%sgw: %s%s", gx[0] ? "; " : "", class_wgrad(D, fo) ? "wgrad3x3 stride 2 bf16" : L.pack == DELTA_PACK_INT8 ? "wgrad1x1 from int8" :
                      L.pack ? "wgrad1x1 from e4m3" : delta::wgrad_kernel_name(fa),
-                     wgrad_aside(L, fa) ? ", second stream" : ", compute stream");
+                     goes_aside(D, fa) ? ", second stream" : ", compute stream");
     }
     snprintf(out, (size_t)cap, "%s%s", gx, gw);
     return DELTA_OK;

@@ -64,20 +64,23 @@ __device__ __forceinline__ u32x2 encode(const float (&v)[8], float inv) {
     }
     return o;
 }
+// Two of a word's four values (the upper two if `hi`), times a scale each.
 template <int FMT>
-__device__ __forceinline__ void decode4(uint32_t w, float s, float *v) {
+__device__ __forceinline__ void decode2(uint32_t w, bool hi, float s0, float s1, float *v) {
     if constexpr (FMT == PACK_INT8) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(w >> (8 * i)) * s;
+        v[0] = (float)(int8_t)(w >> (hi ? 16 : 0)) * s0;
+        v[1] = (float)(int8_t)(w >> (hi ? 24 : 8)) * s1;
     } else {
-        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-        v[0] = a.x * s; v[1] = a.y * s; v[2] = b.x * s; v[3] = b.y * s;
+        const f32x2 a = hi ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+        v[0] = a.x * s0;
+        v[1] = a.y * s1;
     }
 }
+// Eight values of one block.
 template <int FMT>
 __device__ __forceinline__ void decode(u32x2 w, float s, float (&v)[8]) {
-    decode4<FMT>(w.x, s, v);
-    decode4<FMT>(w.y, s, v + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) decode2<FMT>(w[i >> 1], i & 1, s, s, v + 2 * i);
 }
 
 }  // namespace packed
