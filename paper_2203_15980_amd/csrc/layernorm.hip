@@ -23,9 +23,12 @@ namespace ln {
 using packed::u32x2;
 using rows::f32x4;
 
-constexpr int kWaves = 8;                                // of a workgroup that has a row to each wavefront
-constexpr int kRowChannels = 2048, kMostChannels = 8192;          // forward: a wavefront owns a row up to the first
-constexpr int kBackwardRowChannels = 1024;               // backward
+constexpr int kRowChannels = 2048, kMostChannels = 8192; // forward: a wavefront owns a row up to the first
+constexpr int kWaveChannels = 1024;                      // backward: a wavefront owns a row up to here
+// Wavefronts of its workgroup.  The same for a tensor and its checkpoint, with and without gx_add: the sums' order, and so their bits, do not depend on those.
+template <int R> constexpr int kWaves = R == 1 ? 16 : 8;
+
+constexpr int kDeep = 1, kDeepWide = 2;                  // rows fetched ahead, by a wavefront, by a workgroup
 
 struct Args {
     const unsigned char *x, *gy, *add;                   // add: null or [rows, C]
@@ -41,7 +44,7 @@ struct Args {
 template <typename T, int FMT> struct Source {
     rows::Eight<T> v;
     __device__ __forceinline__ void zero() { v.zero(); }
-    __device__ __forceinline__ void load(const Args &a, uint32_t row, uint32_t ck) { v.load(a.x + ((uint64_t)row * a.C + ck * 8) * sizeof(T)); }
+    __device__ __forceinline__ void load(const Args &a, uint32_t row, uint32_t ck) { v.load(a.x + (uint64_t)row * a.C * sizeof(T) + ck * (8u * (uint32_t)sizeof(T))); }
     __device__ __forceinline__ void to(float (&f)[8]) const { v.to(f); }
 };
 template <typename T> struct Packed {
@@ -49,8 +52,8 @@ template <typename T> struct Packed {
     uint32_t byte;
     __device__ __forceinline__ void zero() { q = u32x2{0u, 0u}; byte = 0; }
     __device__ __forceinline__ void load(const Args &a, uint32_t row, uint32_t ck) {
-        q = *reinterpret_cast<const u32x2 *>(a.x + (uint64_t)row * a.C + ck * 8);
-        byte = a.x[a.scales + (uint64_t)row * ((a.C + 31) / 32) + ck / 4];
+        q = *reinterpret_cast<const u32x2 *>(a.x + (uint64_t)row * a.C + ck * 8u);
+        byte = (a.x + a.scales + (uint64_t)row * ((a.C + 31) / 32))[ck / 4];
     }
 };
 template <typename T> struct Source<T, PACK_INT8> : Packed<T> {
@@ -96,29 +99,33 @@ struct GroupSum {
     }
 };
 
-// x of a row into xh; returns 1 / sqrt(var + eps).  Channels past the row's end come as zeros and stay zeros.
+// A product that no neighbouring sum takes in: which product of two a sum is fused with is the compiler's choice, and another one from a checkpoint than
+// from the tensor would give other bits.
+__device__ __forceinline__ float scaled(float v, float by) {
+#pragma clang fp contract(off)
+    return v * by;
+}
+
+// x of a row into x - mean (`over`: 1 / C); returns 1 / sqrt(var + eps).  Channels past the row's end come as zeros and stay zeros.
 template <int R, typename SUM>
-__device__ __forceinline__ float normalise(float (&v)[R][8], const bool (&live)[R], const Args &a, const SUM &sum, float *slots) {
+__device__ __forceinline__ float centre(float (&v)[R][8], const bool (&live)[R], const Args &a, float over, const SUM &sum, float *slots) {
     float s = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int e = 0; e < 8; e += 2) s += v[r][e] + v[r][e + 1];
-    const float mean = sum.one(s, slots) / (float)a.C;
+    const float mean = scaled(sum.one(s, slots), over);
     float sq = 0.f;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        const float m = live[r] ? mean : 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[r][e] = live[r] ? v[r][e] - mean : 0.f;
+            v[r][e] -= m;
             sq += v[r][e] * v[r][e];
         }
-    const float rstd = 1.0f / sqrtf(sum.one(sq, slots + 16) / (float)a.C + a.eps);
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[r][e] *= rstd;
-    return rstd;
+    }
+    return 1.0f / sqrtf(scaled(sum.one(sq, slots + 16), over) + a.eps);
 }
 
 // ---- forward
@@ -127,16 +134,22 @@ __device__ __forceinline__ void forward_rows(const Args &a, uint32_t row, uint32
     bool live[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) live[r] = (ck0 + 64 * r) * 8 < a.C;
+    const float over = 1.0f / (float)a.C;
+    rows::Eight<T> raw[R];
+    auto fetch = [&](uint32_t m) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (live[r]) raw[r].load(a.x + (uint64_t)m * a.C * sizeof(T) + (ck0 + 64 * r) * (8u * (uint32_t)sizeof(T)));
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) raw[r].zero();
+    if (row < a.rows) fetch(row);
     for (; row < a.rows; row += step) {
         float v[R][8];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            rows::Eight<T> raw;
-            raw.zero();
-            if (live[r]) raw.load(a.x + ((uint64_t)row * a.C + (ck0 + 64 * r) * 8) * sizeof(T));
-            raw.to(v[r]);
-        }
-        normalise<R>(v, live, a, sum, slots);
+        for (int r = 0; r < R; ++r) raw[r].to(v[r]);
+        if (row + step < a.rows) fetch(row + step);
+        const float rstd = centre<R>(v, live, a, over, sum, slots);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (!live[r]) continue;
@@ -144,15 +157,15 @@ __device__ __forceinline__ void forward_rows(const Args &a, uint32_t row, uint32
             load8(a.gamma + (ck0 + 64 * r) * 8, g);
             load8(a.beta + (ck0 + 64 * r) * 8, b);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[r][e] = v[r][e] * g[e] + b[e];
-            rows::Eight<T>::store(a.y + ((uint64_t)row * a.C + (ck0 + 64 * r) * 8) * sizeof(T), v[r]);
+            for (int e = 0; e < 8; ++e) v[r][e] = v[r][e] * rstd * g[e] + b[e];
+            rows::Eight<T>::store(a.y + (uint64_t)row * a.C * sizeof(T) + (ck0 + 64 * r) * (8u * (uint32_t)sizeof(T)), v[r]);
         }
     }
 }
 
 template <typename T, int R>
 __global__ __launch_bounds__(256) void forward_kernel(Args a) {
-    forward_rows<T, R>(a, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4, threadIdx.x & 63, WaveSum(), nullptr);
+    forward_rows<T, R>(a, blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), gridDim.x * 4, threadIdx.x & 63, WaveSum(), nullptr);
 }
 template <typename T>
 __global__ __launch_bounds__(1024) void forward_wide_kernel(Args a) {
@@ -161,59 +174,71 @@ __global__ __launch_bounds__(1024) void forward_wide_kernel(Args a) {
 }
 
 // ---- backward
-// ADD: with gx_add.  (Its row is not fetched ahead: at two pieces a lane the registers of four wavefronts on a SIMD would not hold it.)
-template <typename T, int FMT, bool ADD, int R, typename SUM>
-__device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint32_t step, uint32_t ck0, const SUM &sum, float *slots,
+// ADD: with gx_add.  STRIDE: pieces (of eight channels) between two of a thread's.  LDS: `gamma` is the whole row's, in
+// LDS, zeros behind it; else gamma is kept in registers.  DEEP: rows fetched ahead (not of
+// gx_add).
+template <typename T, int FMT, bool ADD, bool LDS, int R, int STRIDE, int DEEP, typename SUM>
+__device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint32_t step, uint32_t ck0, const SUM &sum, float *slots, const float *gamma,
                                               float (&dg)[R][8], float (&db)[R][8]) {
     bool live[R];
-    float gamma[R][8];
+    float kept[8];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        live[r] = (ck0 + 64 * r) * 8 < a.C;
+        live[r] = (ck0 + STRIDE * r) * 8 < a.C;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) gamma[r][e] = dg[r][e] = db[r][e] = 0.f;
-        if (live[r]) load8(a.gamma + (ck0 + 64 * r) * 8, gamma[r]);
+        for (int e = 0; e < 8; ++e) kept[e] = dg[r][e] = db[r][e] = 0.f;
     }
-    Source<T, FMT> xr[R];
-    rows::Eight<T> gr[R];
-    auto fetch = [&](uint32_t m) {
+    if (!LDS && live[0]) load8(a.gamma + ck0 * 8, kept);
+    Source<T, FMT> xr[DEEP][R];
+    rows::Eight<T> gr[DEEP][R];
+    auto fetch = [&](uint32_t m, int d) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (!live[r]) continue;
-            xr[r].load(a, m, ck0 + 64 * r);
-            gr[r].load(a.gy + ((uint64_t)m * a.C + (ck0 + 64 * r) * 8) * sizeof(T));
+            xr[d][r].load(a, m, ck0 + STRIDE * r);
+            gr[d][r].load(a.gy + (uint64_t)m * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)));
         }
     };
 #pragma unroll
-    for (int r = 0; r < R; ++r) { xr[r].zero(); gr[r].zero(); }
-    if (row < a.rows) fetch(row);
+    for (int d = 0; d < DEEP; ++d) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) { xr[d][r].zero(); gr[d][r].zero(); }
+        if (row + d * step < a.rows) fetch(row + d * step, d);
+    }
     const float over = 1.0f / (float)a.C;
-    for (; row < a.rows; row += step) {
-        float x[R][8], gy[R][8];
-        rows::Eight<T> ar[R];
+    auto work = [&](uint32_t row, int d) {
+        // with c = x - mean and u = gy * rstd * gamma: gx = u - mean(u) - c * rstd^2 * mean(u * c), and gy * xh = gy * rstd * c
+        float c[R][8], u[R][8];
+        rows::Eight<T> gc[R], ar[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            xr[r].to(x[r]);
-            gr[r].to(gy[r]);
-            if (ADD && live[r]) ar[r].load(a.add + ((uint64_t)row * a.C + (ck0 + 64 * r) * 8) * sizeof(T));
+            xr[d][r].to(c[r]);
+            gc[r] = gr[d][r];
+            if (ADD && live[r]) ar[r].load(a.add + (uint64_t)row * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)));
         }
-        if (row + step < a.rows) fetch(row + step);
-        const float rstd = normalise<R>(x, live, a, sum, slots);
+        if (row + DEEP * step < a.rows) fetch(row + DEEP * step, d);
+        const float rstd = centre<R>(c, live, a, over, sum, slots);
         float s1 = 0.f, s2 = 0.f;
+        if (LDS) asm volatile("" ::: "memory");          // gamma is read again for each row: kept in registers it would cost a row in flight
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) {
+            float gy[8], gm[8];
+            gc[r].to(gy);
+            if constexpr (LDS) load8(gamma + (ck0 + STRIDE * r) * 8, gm);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                dg[r][e] += gy[r][e] * x[r][e];
-                db[r][e] += gy[r][e];
-                gy[r][e] *= gamma[r][e];
-                s1 += gy[r][e];
-                s2 += gy[r][e] * x[r][e];
+                const float t = scaled(gy[e], rstd);
+                dg[r][e] += t * c[r][e];
+                db[r][e] += gy[e];
+                u[r][e] = scaled(t, LDS ? gm[e] : kept[e]);
+                s1 += u[r][e];
+                s2 += u[r][e] * c[r][e];
             }
+        }
         sum.two(s1, s2, slots + 32);
-        if (!a.gx) continue;
-        s1 *= over;
-        s2 *= over;
+        if (!a.gx) return;
+        s1 = scaled(s1, over);
+        s2 = scaled(scaled(s2, over), scaled(rstd, rstd));
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (!live[r]) continue;
@@ -221,34 +246,42 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
             if constexpr (ADD) ar[r].to(add);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                o[e] = rstd * (gy[r][e] - s1 - x[r][e] * s2);
+                o[e] = (u[r][e] - s1) - c[r][e] * s2;
                 if constexpr (ADD) o[e] += add[e];
             }
-            rows::Eight<T>::store(a.gx + ((uint64_t)row * a.C + (ck0 + 64 * r) * 8) * sizeof(T), o);
+            rows::Eight<T>::store(a.gx + (uint64_t)row * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)), o);
         }
-    }
+    };
+#pragma unroll 1
+    for (; row < a.rows; row += DEEP * step)
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d)
+            if (row + d * step < a.rows) work(row + d * step, d);
 }
 
-// A row to a wavefront, R * 512 channels; the wavefronts' sums meet in LDS, [kWaves][C], in their order.
+// A row to a wavefront, R * 512 channels; the wavefronts' sums meet in LDS, [wavefronts][C], in their order.
 template <typename T, int FMT, bool ADD, int R>
-__global__ __launch_bounds__(kWaves * 64, R == 1 ? 4 : 2) void backward_kernel(Args a) {
-    extern __shared__ __align__(16) float red[];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(kWaves<R> * 64) void backward_kernel(Args a) {
+    constexpr int W = kWaves<R>;
+    extern __shared__ __align__(16) float shared[];
+    const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    for (uint32_t c = threadIdx.x; c < R * 512; c += W * 64) shared[c] = c < a.C ? a.gamma[c] : 0.f;
+    __syncthreads();
     float dg[R][8], db[R][8];
-    backward_rows<T, FMT, ADD, R>(a, blockIdx.x * kWaves + wave, gridDim.x * kWaves, lane, WaveSum(), nullptr, dg, db);
+    backward_rows<T, FMT, ADD, true, R, 64, kDeep>(a, blockIdx.x * W + wave, gridDim.x * W, lane, WaveSum(), nullptr, shared, dg, db);
     if (!a.partial) return;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        if (half) __syncthreads();                       // the first half's sums are read
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();                                 // gamma, then the first sums, are read
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if ((lane + 64 * r) * 8 < a.C) store8(red + wave * a.C + (lane + 64 * r) * 8, half ? db[r] : dg[r]);
+            if ((lane + 64 * r) * 8 < a.C) store8(shared + wave * a.C + (lane + 64 * r) * 8, which ? db[r] : dg[r]);
         __syncthreads();
-        for (uint32_t c = threadIdx.x; c < a.C; c += kWaves * 64) {
+        for (uint32_t c = threadIdx.x; c < a.C; c += W * 64) {
             float s = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) s += red[w * a.C + c];
-            a.partial[((uint64_t)blockIdx.x * 2 + half) * a.C + c] = s;
+            for (int w = 0; w < W; ++w) s += shared[w * a.C + c];
+            a.partial[((uint64_t)blockIdx.x * 2 + which) * a.C + c] = s;
         }
     }
 }
@@ -257,7 +290,7 @@ template <typename T, int FMT, bool ADD>
 __global__ __launch_bounds__(1024) void backward_wide_kernel(Args a) {
     __shared__ float slots[64];
     float dg[1][8], db[1][8];
-    backward_rows<T, FMT, ADD, 1>(a, blockIdx.x, gridDim.x, threadIdx.x, GroupSum{(int)(threadIdx.x >> 6), (int)(blockDim.x >> 6)}, slots, dg, db);
+    backward_rows<T, FMT, ADD, false, 1, 1, kDeepWide>(a, blockIdx.x, gridDim.x, threadIdx.x, GroupSum{(int)(threadIdx.x >> 6), (int)(blockDim.x >> 6)}, slots, nullptr, dg, db);
     if (!a.partial || threadIdx.x * 8 >= a.C) return;
     store8(a.partial + (uint64_t)blockIdx.x * 2 * a.C + threadIdx.x * 8, dg[0]);
     store8(a.partial + ((uint64_t)blockIdx.x * 2 + 1) * a.C + threadIdx.x * 8, db[0]);
@@ -286,7 +319,7 @@ __global__ __launch_bounds__(1024) void partials_kernel(const float *partial, fl
 
 // Workgroups of the backward launch: as many as are resident at once, and no more than there are rows for.
 uint32_t workgroups(long long rows, int C) {
-    const long long per = C <= kBackwardRowChannels ? kWaves : 1, most = C <= 4096 ? 512 : 256;
+    const long long per = C <= 512 ? kWaves<1> : C <= kWaveChannels ? kWaves<2> : 1, most = C <= kWaveChannels ? 256 : C <= 4096 ? 512 : 256;
     const long long want = (rows + per - 1) / per;
     return (uint32_t)(want < most ? want : most);
 }
@@ -321,13 +354,16 @@ size_t layernorm_bwd_workspace_bytes(long long rows, int C) { return (size_t)ln:
 
 template <typename T, int FMT, bool ADD>
 static hipError_t layernorm_bwd(const ln::Args &a, uint32_t grid, hipStream_t stream) {
-    if (a.C > ln::kBackwardRowChannels) {
+    if (a.C > ln::kWaveChannels) {
         ln::backward_wide_kernel<T, FMT, ADD><<<dim3(grid), dim3((a.C / 8 + 63) / 64 * 64), 0, stream>>>(a);
         return hipGetLastError();
     }
-    const size_t lds = a.partial ? (size_t)ln::kWaves * a.C * sizeof(float) : 0;         // 32 KB at most
-    if (a.C <= 512) ln::backward_kernel<T, FMT, ADD, 1><<<dim3(grid), dim3(ln::kWaves * 64), lds, stream>>>(a);
-    else ln::backward_kernel<T, FMT, ADD, 2><<<dim3(grid), dim3(ln::kWaves * 64), lds, stream>>>(a);
+    auto run = [&](auto kernel, unsigned waves) {
+        const size_t sums = a.partial ? (size_t)waves * a.C : 0, gamma = (a.C + 511) / 512 * 512;
+        kernel<<<dim3(grid), dim3(waves * 64), (sums > gamma ? sums : gamma) * sizeof(float), stream>>>(a);              // 32 KB at most
+    };
+    if (a.C <= 512) run(ln::backward_kernel<T, FMT, ADD, 1>, ln::kWaves<1>);
+    else run(ln::backward_kernel<T, FMT, ADD, 2>, ln::kWaves<2>);
     return hipGetLastError();
 }
 template <typename T>

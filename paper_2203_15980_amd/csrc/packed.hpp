@@ -64,12 +64,23 @@ __device__ __forceinline__ u32x2 encode(const float (&v)[8], float inv) {
     }
     return o;
 }
+// Byte N of a word, signed, as fp32: one instruction, where the compiler often makes three (layer normalisation's gradients from int8, 768 channels, 16384 rows:
+// 21.3 us, 17 with it).
+template <int N>
+__device__ __forceinline__ float signed_byte(uint32_t w) {
+    float f;
+    if constexpr (N == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
+    if constexpr (N == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
+    if constexpr (N == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
+    if constexpr (N == 3) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
+    return f;
+}
 // Two of a word's four values (the upper two if `hi`), times a scale each.
 template <int FMT>
 __device__ __forceinline__ void decode2(uint32_t w, bool hi, float s0, float s1, float *v) {
     if constexpr (FMT == PACK_INT8) {
-        v[0] = (float)(int8_t)(w >> (hi ? 16 : 0)) * s0;
-        v[1] = (float)(int8_t)(w >> (hi ? 24 : 8)) * s1;
+        v[0] = (hi ? signed_byte<2>(w) : signed_byte<0>(w)) * s0;
+        v[1] = (hi ? signed_byte<3>(w) : signed_byte<1>(w)) * s1;
     } else {
         const f32x2 a = hi ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
         v[0] = a.x * s0;

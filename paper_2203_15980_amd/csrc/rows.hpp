@@ -60,16 +60,26 @@ __device__ __forceinline__ float dpp(float v) { return __uint_as_float(dpp<CTRL>
 __device__ __forceinline__ uint32_t quad_xor1(uint32_t v) { return dpp<0xB1>(v); }     // quad_perm 1,0,3,2
 __device__ __forceinline__ uint32_t quad_xor2(uint32_t v) { return dpp<0x4E>(v); }     // quad_perm 2,3,0,1
 
-// The sum of v over the 64 lanes, the same in each: within the rows of 16 by quad permutations and mirrors, then the four rows' sums.  All lanes active.
-__device__ __forceinline__ float wave_sum(float v) {
+// v plus its value in the other row of 16 of each half (the other half) of the wavefront: the swap hands a register's odd rows (upper half) to a copy's
+// even ones (lower half).
+__device__ __forceinline__ float row_pairs(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// The sum of v over the 32 lanes of half a wavefront, over all 64, the same in each: within the rows of 16 by quad permutations and mirrors, then by the
+// swaps.  All lanes of the half (of the wavefront) active.
+__device__ __forceinline__ float half_sum(float v) {
     v += dpp<0xB1>(v);
     v += dpp<0x4E>(v);
     v += dpp<0x141>(v);                                                    // row_half_mirror: the other quad of a lane's eight
     v += dpp<0x140>(v);                                                    // row_mirror: the other eight
-    const int b = (int)__float_as_uint(v);
-    return (__uint_as_float(__builtin_amdgcn_readlane(b, 0)) + __uint_as_float(__builtin_amdgcn_readlane(b, 16))) +
-           (__uint_as_float(__builtin_amdgcn_readlane(b, 32)) + __uint_as_float(__builtin_amdgcn_readlane(b, 48)));
+    return row_pairs(v);
 }
+__device__ __forceinline__ float wave_sum(float v) { return halves(half_sum(v)); }
 
 }  // namespace rows
 }  // namespace delta
