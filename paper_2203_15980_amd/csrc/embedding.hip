@@ -7,9 +7,9 @@
 // Gradient: rows of gw from the tokens in sorted order; no atomics on values, so the sums' order is fixed by the ids alone.  What bounds it is the write
 // of gw (4 V C bytes) beside one read of gy.
 //   * sort, and zeros beside it: gw is filled with zeros by the launches that sort, whose few workgroups leave the memory idle; rows of ids that occur are
-//     written once more (never more than there are tokens).  Up to kOneGroup tokens one workgroup sorts (id, position) pairs in
-//     LDS; beyond, a stable radix sort of two digits over all workgroups: each ranks kSortItems tokens by ballots within a wavefront
-//     and finds its bases from all workgroups' digit counts itself.
+//     written once more (never more than there are tokens).  Up to kInLds tokens one workgroup sorts (id, position) pairs in LDS; beyond, a stable
+//     radix sort of two digits over all workgroups: each ranks kSortItems tokens by ballots within a wavefront and finds its bases from all
+//     workgroups' digit counts itself.  (One workgroup for 16384 tokens, or sixteen with an id's low bits each, took 23 us where the four launches take 20.)
 //   * sums: a workgroup owns a chunk of sorted places, whose rows of gy it fetches 16 (fp32: 8) at a time, and adds up run by run.  A run of one id
 //     that begins and ends in the chunk is a row of gw; what a chunk holds of a run that goes on beyond it becomes a partial sum: its first run in slot 0
 //     if it came in from the chunk before, its last in slot 1 if it began here.  However often an id occurs, a chain is a chunk long.
@@ -26,7 +26,7 @@ namespace emb {
 using rows::f32x4;
 
 constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup, chunks of the joins
-constexpr uint32_t kOneGroup = 16384;                    // most tokens that one workgroup sorts: 16 to a thread (64-bit items: a quarter)
+constexpr uint32_t kInLds = 1024;                        // most tokens that one workgroup sorts in LDS
 constexpr uint32_t kSortItems = 1024;                    // of a workgroup in the sort over all: 4 wavefronts, 4 rounds of 64 each
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
 constexpr long long kMostTokens = 1 << 24;
@@ -93,9 +93,6 @@ struct Plan {
     uint64_t key1, pos1, key2, pos2, hist1, hist2, sums, bytes;                    // workspace: byte offsets and size
 };
 
-// Whether one workgroup sorts all tokens.
-inline bool one_group(uint32_t n, uint32_t bits) { return n <= (bits + 14 > 32 ? kOneGroup / 4 : kOneGroup); }
-
 Plan plan_for(long long n, int V, int C) {
     Plan p;
     p.n = (uint32_t)n; p.V = (uint32_t)V; p.C = (uint32_t)C;
@@ -108,7 +105,7 @@ Plan plan_for(long long n, int V, int C) {
     p.chunks = (p.n + p.chunk - 1) / p.chunk;
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const bool one = one_group(p.n, p.bits);
+    const bool one = p.n <= kInLds;
     p.key1 = take(one ? 0 : 4ull * p.n); p.pos1 = take(one ? 0 : 4ull * p.n);
     p.key2 = take(4ull * p.n); p.pos2 = take(4ull * p.n);
     p.hist1 = take(one ? 0 : (4ull << p.bits1) * p.blocks); p.hist2 = take(one ? 0 : (4ull << p.bits2) * p.blocks);
@@ -129,11 +126,11 @@ struct Args {
 
 __device__ __forceinline__ uint32_t key_of(int64_t id, uint32_t V) { return (uint64_t)id < V ? (uint32_t)id : V; }
 
-// Part `part` of `parts` of gw filled with zeros by the workgroups from `from` on.
-__device__ __forceinline__ void fill(const Args &a, uint32_t from, uint32_t part, uint32_t parts) {
-    const uint64_t pieces = (uint64_t)a.V * a.C / 4, lo = pieces / parts * part, hi = part + 1 == parts ? pieces : pieces / parts * (part + 1);
+// The eighths [lo, hi) of gw filled with zeros by the workgroups from `from` on.
+__device__ __forceinline__ void fill(const Args &a, uint32_t from, uint32_t lo, uint32_t hi) {
+    const uint64_t pieces = (uint64_t)a.V * a.C / 4, first = pieces * lo / 8, end = pieces * hi / 8;
     f32x4 *p = reinterpret_cast<f32x4 *>(a.gw);
-    for (uint64_t i = lo + (uint64_t)(blockIdx.x - from) * blockDim.x + threadIdx.x; i < hi; i += (uint64_t)(gridDim.x - from) * blockDim.x)
+    for (uint64_t i = first + (uint64_t)(blockIdx.x - from) * blockDim.x + threadIdx.x; i < end; i += (uint64_t)(gridDim.x - from) * blockDim.x)
         p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
@@ -147,48 +144,61 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, uint32_t bits, bool l
     return same;
 }
 
-// Workgroup 0 sorts all tokens; the others fill gw.  T: (id, position) in 32 or 64 bits, the position in the low 14.  A thread holds ITEMS neighbouring
-// items; a pass (at most 5 bits) counts each thread's digits in a column of its own, sums the counts by (digit, thread), which is the sorted order of
-// equal digits, and moves each item to its count's sum.  Every 16th word of LDS is followed by an unused one: a thread's words lie side by side.
-template <typename T, int ITEMS, int THREADS>
+// LDS of the sort in one workgroup: four neighbouring items to a thread.  Every 16th word is followed by an unused one: a thread's words lie side by side.
 struct SortLds {
-    T item[ITEMS * THREADS * 17 / 16];
-    uint32_t count[THREADS * 16 * 17 / 16];              // two counts to a word, [digit][thread]
-    uint32_t part[THREADS / 64];
+    uint32_t item[kInLds * 17 / 16];
+    uint32_t count[256 * 16 * 17 / 16];                  // two counts to a word, [digit][thread]
+    uint32_t part[4];
 };
 __device__ __forceinline__ uint32_t spaced(uint32_t i) { return i + (i >> 4); }
 
-template <typename T, int ITEMS, int THREADS>
-__global__ __launch_bounds__(THREADS) void sort_kernel(Args a) {
+// The sum of v over the 256 threads' before this one; `part`: a word to a wavefront.
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *part) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t run = v;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t u = __shfl_up(run, o, 64);
+        if ((int)lane >= o) run += u;
+    }
+    if (lane == 63) part[wave] = run;
+    __syncthreads();
+    run -= v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) run += (uint32_t)i < wave ? part[i] : 0;
+    return run;
+}
+
+// Workgroup 0 sorts all tokens, the others fill gw.  An item is an id above its position, in 32 bits.  A pass (at most 5 bits) counts each thread's digits in a
+// column of its own, sums the counts by (digit, thread), which is the sorted order of equal digits, and moves each item to its count's sum.
+__global__ __launch_bounds__(256) void sort_kernel(Args a) {
+    constexpr uint32_t kPlaceBits = 10, kItems = 4;
+    static_assert(kInLds == 1u << kPlaceBits && kInLds == kItems * 256 && kPlaceBits + kMostBits <= 32, "an item is 32 bits");
     if (blockIdx.x) {
-        fill(a, 1, 0, 1);
+        fill(a, 1, 0, 8);
         return;
     }
-    extern __shared__ __align__(16) unsigned char smem[];
-    SortLds<T, ITEMS, THREADS> &l = *reinterpret_cast<SortLds<T, ITEMS, THREADS> *>(smem);
+    __shared__ SortLds l;
     uint16_t *const count = reinterpret_cast<uint16_t *>(l.count);
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    T item[ITEMS];
+    const uint32_t tid = threadIdx.x;
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        const uint32_t i = tid + k * THREADS;
-        item[k] = i < a.n ? (T)key_of(a.id[i], a.V) << 14 | i : ~(T)0;    // what is behind the last token sorts behind it: all its bits are set
+    for (uint32_t k = 0; k < kItems; ++k) {              // what is behind the last token sorts behind it: all its bits are set, and it comes last
+        const uint32_t i = tid + k * 256;
+        l.item[spaced(i)] = i < a.n ? key_of(a.id[i], a.V) << kPlaceBits | i : ~0u;
     }
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) l.item[spaced(tid + k * THREADS)] = item[k];
     const uint32_t passes = (a.bits + 4) / 5, width = (a.bits + passes - 1) / passes, words = (1u << width) / 2;     // words of counts a thread sums
     const uint32_t column = spaced(tid / 2) * 2 + (tid & 1);
-    auto at = [&](uint32_t d) { return d * (THREADS * 17 / 16) + column; };         // spaced(d * THREADS / 2 + tid / 2): THREADS / 2 is a multiple of 16
+    auto at = [&](uint32_t d) { return d * (256 * 17 / 16) + column; };             // spaced(d * 128 + tid / 2)
     for (uint32_t p = 0; p < passes; ++p) {
-        const uint32_t shift = 14 + p * width, mask = (1u << width) - 1;
-        for (uint32_t i = tid; i < spaced(words * THREADS); i += THREADS) l.count[i] = 0;
+        const uint32_t shift = kPlaceBits + p * width, mask = (1u << width) - 1;
+        for (uint32_t i = tid; i < spaced(words * 256); i += 256) l.count[i] = 0;
         __syncthreads();
-        uint32_t rank[ITEMS];
+        uint32_t item[kItems], rank[kItems];
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) item[k] = l.item[spaced(tid * ITEMS + k)];
+        for (uint32_t k = 0; k < kItems; ++k) item[k] = l.item[spaced(tid * kItems + k)];
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t i = at((uint32_t)(item[k] >> shift) & mask);
+        for (uint32_t k = 0; k < kItems; ++k) {
+            const uint32_t i = at(item[k] >> shift & mask);
             rank[k] = count[i];
             count[i] = (uint16_t)(rank[k] + 1);
         }
@@ -199,17 +209,7 @@ __global__ __launch_bounds__(THREADS) void sort_kernel(Args a) {
             w[j] = (uint32_t)j < words ? l.count[spaced(tid * words + j)] : 0;
             sum += (w[j] & 0xFFFFu) + (w[j] >> 16);
         }
-        uint32_t run = sum;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const uint32_t v = __shfl_up(run, o, 64);
-            if ((int)lane >= o) run += v;
-        }
-        if (lane == 63) l.part[wave] = run;
-        __syncthreads();
-        run -= sum;
-#pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) run += (uint32_t)i < wave ? l.part[i] : 0;
+        uint32_t run = sum_before(sum, l.part);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             if ((uint32_t)j >= words) break;
@@ -219,13 +219,13 @@ __global__ __launch_bounds__(THREADS) void sort_kernel(Args a) {
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) l.item[spaced(count[at((uint32_t)(item[k] >> shift) & mask)] + rank[k])] = item[k];
+        for (uint32_t k = 0; k < kItems; ++k) l.item[spaced(count[at(item[k] >> shift & mask)] + rank[k])] = item[k];
         __syncthreads();
     }
-    for (uint32_t i = tid; i < a.n; i += THREADS) {
-        const T v = l.item[spaced(i)];
-        a.key2[i] = (uint32_t)(v >> 14);
-        a.pos2[i] = (uint32_t)v & 16383u;
+    for (uint32_t i = tid; i < a.n; i += 256) {
+        const uint32_t v = l.item[spaced(i)];
+        a.key2[i] = v >> kPlaceBits;
+        a.pos2[i] = v & (kInLds - 1);
     }
 }
 
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(THREADS) void sort_kernel(Args a) {
 template <bool FIRST>
 __global__ __launch_bounds__(256) void count_kernel(Args a) {
     if (blockIdx.x >= a.blocks) {
-        fill(a, a.blocks, FIRST ? 0 : 2, 4);
+        fill(a, a.blocks, FIRST ? 0 : 4, FIRST ? 1 : 5);           // counting is over in half a scatter's time
         return;
     }
     __shared__ uint32_t bins[kMostBins];
@@ -254,28 +254,37 @@ __global__ __launch_bounds__(256) void count_kernel(Args a) {
 template <bool FIRST>
 __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     if (blockIdx.x >= a.blocks) {
-        fill(a, a.blocks, FIRST ? 1 : 3, 4);
+        fill(a, a.blocks, FIRST ? 1 : 5, FIRST ? 4 : 8);
         return;
     }
     __shared__ uint32_t base[kMostBins];                 // where this workgroup's tokens of a digit begin
     __shared__ uint32_t mine[4][kMostBins];              // tokens of a digit in each wavefront; then in those before it
-    __shared__ uint32_t part[256];
+    __shared__ uint32_t part[4];
+    constexpr int kRounds = kSortItems / 256;
     const uint32_t bits = FIRST ? a.bits1 : a.bits2, shift = FIRST ? 0 : a.bits1, nbins = 1u << bits;
     const uint32_t *hist = FIRST ? a.hist1 : a.hist2;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (uint32_t i = tid; i < 4 * nbins; i += 256) mine[i / nbins][i % nbins] = 0;
+    const uint32_t i0 = blockIdx.x * kSortItems + wave * (kSortItems / 4);
+    uint32_t key[kRounds], pos[kRounds], rank[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const uint32_t i = i0 + r * 64 + lane;
+        key[r] = 0; pos[r] = i;
+        if (i >= a.n) continue;
+        key[r] = FIRST ? key_of(a.id[i], a.V) : a.key1[i];
+        if (!FIRST) pos[r] = a.pos1[i];
+    }
+    for (uint32_t w = 0; w < 4; ++w)
+        for (uint32_t i = tid; i < nbins; i += 256) mine[w][i] = 0;
     // all tokens of smaller digits, and this digit's in the workgroups before: a thread sums its share of the digits, each over the workgroups
     const uint32_t per = (nbins + 255) / 256;
-    uint32_t before[kMostBins / 256], sum = 0;
-#pragma unroll
-    for (int k = 0; k < kMostBins / 256; ++k) before[k] = 0;
-    uint32_t all[kMostBins / 256];
+    uint32_t before[kMostBins / 256], all[kMostBins / 256], sum = 0;
 #pragma unroll
     for (int k = 0; k < kMostBins / 256; ++k) {
         const uint32_t d = tid * per + k;
-        all[k] = 0;
+        before[k] = all[k] = 0;
         if ((uint32_t)k >= per || d >= nbins) continue;
-#pragma unroll 8
+#pragma unroll 16
         for (uint32_t b = 0; b < a.blocks; ++b) {
             const uint32_t c = hist[(uint64_t)b * nbins + d];
             before[k] += b < blockIdx.x ? c : 0;
@@ -283,15 +292,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
         }
         sum += all[k];
     }
-    part[tid] = sum;
-    __syncthreads();
-    for (uint32_t o = 1; o < 256; o *= 2) {              // inclusive sums over the threads
-        const uint32_t v = tid >= o ? part[tid - o] : 0;
-        __syncthreads();
-        part[tid] += v;
-        __syncthreads();
-    }
-    uint32_t run = part[tid] - sum;
+    uint32_t run = sum_before(sum, part);
 #pragma unroll
     for (int k = 0; k < kMostBins / 256; ++k) {
         const uint32_t d = tid * per + k;
@@ -299,18 +300,10 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
         base[d] = run + before[k];
         run += all[k];
     }
-    // ranks within a wavefront: how many lanes before hold the same digit, after the rounds before
-    const uint32_t i0 = blockIdx.x * kSortItems + wave * (kSortItems / 4);
-    uint32_t key[kSortItems / 256], pos[kSortItems / 256], rank[kSortItems / 256];
+    // ranks within a wavefront: how many lanes before hold the same digit, after the rounds before (`mine` is cleared: sum_before has a barrier)
 #pragma unroll
-    for (int r = 0; r < (int)(kSortItems / 256); ++r) {
-        const uint32_t i = i0 + r * 64 + lane;
-        const bool live = i < a.n;
-        key[r] = 0; pos[r] = i;
-        if (live) {
-            key[r] = FIRST ? key_of(a.id[i], a.V) : a.key1[i];
-            if (!FIRST) pos[r] = a.pos1[i];
-        }
+    for (int r = 0; r < kRounds; ++r) {
+        const bool live = i0 + r * 64 + lane < a.n;
         const uint32_t d = (key[r] >> shift) & (nbins - 1);
         const uint64_t same = same_digit(d, bits, live);
         const uint32_t lower = (uint32_t)__popcll(same & ((1ull << lane) - 1));
@@ -333,7 +326,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < (int)(kSortItems / 256); ++r) {
+    for (int r = 0; r < kRounds; ++r) {
         if (i0 + r * 64 + lane >= a.n) continue;
         const uint32_t to = mine[wave][(key[r] >> shift) & (nbins - 1)] + rank[r];
         if (FIRST) {
@@ -481,36 +474,22 @@ hipError_t launch_embedding(const void *id, const void *w, const float *scale, v
 size_t embedding_bwd_workspace_bytes(long long n, int V, int C) { return emb::plan_for(n, V, C).bytes; }
 
 // Workgroups that fill gw beside a sort: enough to keep the memory busy, no more than there is work for.
-static uint32_t fillers(const emb::Args &a, uint32_t threads, uint32_t parts) {
-    const uint64_t want = (uint64_t)a.V * a.C / 4 / parts / (threads * 4) + 1, most = 2048 * 256 / threads;
+static uint32_t fillers(const emb::Args &a, uint32_t eighths) {
+    const uint64_t want = (uint64_t)a.V * a.C / 4 * eighths / 8 / (256 * 4) + 1, most = 2048;
     return (uint32_t)(want < most ? want : most);
-}
-
-template <typename T, int ITEMS, int THREADS>
-static hipError_t embedding_sort(const emb::Args &a, hipStream_t stream) {
-    const int lds = (int)sizeof(emb::SortLds<T, ITEMS, THREADS>);
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&emb::sort_kernel<T, ITEMS, THREADS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    emb::sort_kernel<T, ITEMS, THREADS><<<dim3(1 + fillers(a, THREADS, 1)), dim3(THREADS), lds, stream>>>(a);
-    return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t embedding_bwd(const emb::Args &a, hipStream_t stream) {
     using namespace emb;
-    if (one_group(a.n, a.bits)) {
-        const bool wide = a.bits + 14 > 32;
-        hipError_t e;
-        if (a.n <= 1024) e = wide ? embedding_sort<uint64_t, 4, 256>(a, stream) : embedding_sort<uint32_t, 4, 256>(a, stream);
-        else if (a.n <= 4096) e = wide ? embedding_sort<uint64_t, 4, 1024>(a, stream) : embedding_sort<uint32_t, 4, 1024>(a, stream);
-        else e = embedding_sort<uint32_t, 16, 1024>(a, stream);
-        if (e != hipSuccess) return e;
+    if (a.n <= kInLds) {
+        sort_kernel<<<dim3(1 + fillers(a, 8)), dim3(256), 0, stream>>>(a);
     } else {
-        const dim3 grid(a.blocks + fillers(a, 256, 4)), block(256);
-        count_kernel<true><<<grid, block, 0, stream>>>(a);
-        scatter_kernel<true><<<grid, block, 0, stream>>>(a);
-        count_kernel<false><<<grid, block, 0, stream>>>(a);
-        scatter_kernel<false><<<grid, block, 0, stream>>>(a);
+        const dim3 counting(a.blocks + fillers(a, 1)), scattering(a.blocks + fillers(a, 3)), block(256);
+        count_kernel<true><<<counting, block, 0, stream>>>(a);
+        scatter_kernel<true><<<scattering, block, 0, stream>>>(a);
+        count_kernel<false><<<counting, block, 0, stream>>>(a);
+        scatter_kernel<false><<<scattering, block, 0, stream>>>(a);
     }
     const uint32_t threads = (a.pieces + 63) / 64 * 64;
     sums_kernel<T, sizeof(T) == 2 ? 16 : 8><<<dim3(a.chunks), dim3(threads), 0, stream>>>(a);
