@@ -8,11 +8,14 @@
 //  * x stays in 8 bits as far as the registers: gfx950's transposing read of bytes (ds_read_b64_tr_b8: 16 lanes point at 8 rows of 16 channels, each
 //    gets one channel's 8 values along the rows) gives a lane the 8 pixels of one MFMA operand, which it converts: 20 instructions for 8 values in
 //    int8, 16 in E4M3.  So that these hide behind the MFMAs a wavefront owns 128 x 64 of (k, c) where K allows: 8 MFMAs (256 cycles) for
-//    40 conversions (160).  The pixels' scales are turned into fp32 once a slice, a slice ahead, and read by whole wavefronts at once.
+//    40 conversions (160).  The pixels' scales are turned into bf16 once a slice, a slice ahead, and read by whole wavefronts at once (in
+//    fp32 these reads were half of all LDS reads).
 //    With x converted by the whole workgroup into a bf16 tile a slice ahead instead, and 64 x 64 to a wavefront, a slice's steps waited for one
 //    another: 43 us for 768 -> 768 on 16384 tokens.
 //  * Workgroups are numbered so that those of one split, which read the same pixels, are on one XCD and share its L2: a third of the misses.
 //  * The wavefronts that share a tile add their sums through LDS, in a fixed tree.
+// us, and the reduction's beside them: 768 -> 768 on 16384 tokens, int8, 35 + 5.5 (550 TFLOP/s; E4M3 33; wgrad1x1.hip on the unpacked tensor 40 + 5.5), on 333 tokens
+// 1024 -> 256 9 + 2.  Bound by neither memory (38 MB, 6 us) nor the matrix units (8) alone: a slice's waits, LDS reads and conversions beside the products.
 // Rows past the last pixel are fetched from the last pixel and overwritten with zeros in LDS; their scales are zeros.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -45,12 +48,12 @@ template <int KT, int CT> struct Shape {
     static constexpr int kPixels = KT == 4 ? 64 : 128;                                           // of a slice
     static constexpr int kG = kPixels * KT * 128, kX = kPixels * CT * 64;                        // bytes of a slice: gpre, bytes of x
     static constexpr int kScaleWords = CT == 4 ? 2 : 1, kScales = kPixels * kScaleWords * 4;     // 4-byte words of scale bytes a pixel
-    static constexpr int kSlice = kG + kX + kScales, kFloats = CT * 2 * kPixels * 4;             // of the ring; of a slice's scales in fp32
-    static constexpr int kFit = (160 * 1024 - 2 * kFloats) / kSlice, kStages = kFit < 5 ? kFit : 5;
+    static constexpr int kSlice = kG + kX + kScales, kMade = CT * 2 * kPixels * 2;               // of the ring; of a slice's scales in bf16
+    static constexpr int kFit = (160 * 1024 - 2 * kMade) / kSlice, kStages = kFit < 5 ? kFit : 5;
     static constexpr int kGL = kG / 8192, kXB = kX / 1024, kXL = kXB < 8 ? 1 : kXB / 8;          // loads per wavefront; 1 KB blocks of x
     static constexpr int kSB = kScales / 256, kLoads = kGL + kXL + 1;                            // 256-byte blocks of scales
     static constexpr int kSums = kQS / 2 * kTiles * kF * 8192;
-    static constexpr int kRing = kStages * kSlice + 2 * kFloats, kLds = kRing > kSums ? kRing : kSums;
+    static constexpr int kRing = kStages * kSlice + 2 * kMade, kLds = kRing > kSums ? kRing : kSums;
     static_assert(kStages >= 3 && kLds <= 160 * 1024, "one slice multiplied, two in flight");
 };
 
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
     using T = Shape<KT, CT>;
     constexpr int GP = KT * 128, XP = CT * 64, S = T::kStages, QS = T::kQS, F = T::kF;
     extern __shared__ __align__(16) unsigned char smem[];
-    float *const floats = reinterpret_cast<float *>(smem + S * T::kSlice);       // [2][CT * 2 blocks][kPixels]
+    uint16_t *const made = reinterpret_cast<uint16_t *>(smem + S * T::kSlice);   // [2][CT * 2 blocks][kPixels]
     const int tid = threadIdx.x, lane = tid & 63;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int base = wv % T::kTiles, qs = wv / T::kTiles, kw = base % T::kAlong, cw = base / T::kAlong;
@@ -136,17 +139,17 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
         else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * T::kLoads - 1) : "memory");
         else asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * T::kLoads - 1) : "memory");
     };
-    // the scales of a slice in the ring, in fp32, [block][pixel]
-    auto scales = [&](int slice, int buf, float *out) {
+    // the scales of a slice in the ring, in bf16 (a power of two, or NaN), [block][pixel]
+    auto scales = [&](int slice, int buf, uint16_t *out) {
         const int last = a.M - 1 - slice * T::kPixels;
         const unsigned char *raw = smem + buf * T::kSlice + T::kG + T::kX;
 #pragma unroll
-        for (int i = 0; i < (T::kFloats / 4 + 511) / 512; ++i) {
-            const int p = (tid + i * 512) % (T::kFloats / 4), block = p / T::kPixels, pixel = p % T::kPixels;      // fewer scales than threads: some make one twice
+        for (int i = 0; i < (T::kMade / 2 + 511) / 512; ++i) {
+            const int p = (tid + i * 512) % (T::kMade / 2), block = p / T::kPixels, pixel = p % T::kPixels;      // fewer scales than threads: some make one twice
             uint32_t at = (uint32_t)block;
             if constexpr (CT == 1) at += (uint32_t)(((uint64_t)(uint32_t)(slice * T::kPixels + (pixel < last ? pixel : last)) * nb + (uint32_t)(ct * 2)) & 3);
-            const float s = packed::scale_of(raw[pixel * (T::kScaleWords * 4) + at]);
-            out[p] = pixel <= last ? s : 0.f;
+            const uint32_t byte = raw[pixel * (T::kScaleWords * 4) + at];
+            out[p] = (uint16_t)(pixel <= last ? (byte == 255u ? 0x7FC0u : byte << 7) : 0u);
         }
     };
 
@@ -182,7 +185,7 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
         if (t < mine) fetch(slice_of(t), t);
     wait_scales(mine - 1 < S - 2 ? mine - 1 : S - 2);            // those of slice 0
     __syncthreads();
-    scales(slice_of(0), 0, floats);
+    scales(slice_of(0), 0, made);
     for (int t = 0, buf = 0; t < mine; ++t) {
         const int later = mine - 2 - t < S - 3 ? mine - 2 - t : S - 3;
         wait_scales(later);                                      // this wavefront's part of slice t and its scales of slice t + 1 have landed
@@ -198,23 +201,20 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
             }
             __syncthreads();
         }
-        // behind the last slice: of a buffer that nothing reads any more
-        scales(slice_of(t + 1), next, floats + ((t + 1) & 1) * (T::kFloats / 4));
-        const float *sc = floats + (t & 1) * (T::kFloats / 4) + cw * 2 * T::kPixels + 8 * (lane >> 5);
+        const uint16_t *sc = made + (t & 1) * (T::kMade / 2) + cw * 2 * T::kPixels + 8 * (lane >> 5);
         // Step by step: all reads of a step first, then, pair by pair between two MFMAs of the step before (32 cycles, room for eight other instructions),
         // its conversions.  The compiler is held to this order, or it converts a whole step before it multiplies.
         constexpr int kSteps = T::kPixels / (16 * QS);
         s16x8 af[2][F];
         u32x4 bf[2][2];
         i32x2 raw[2];
-        f32x4 sv[2][2];
+        u32x4 sv[2];
         auto read = [&](int q, int to) {
             const int q0 = 16 * (qs + q * QS);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 raw[h] = tr_read8(sl + q0 * XP + xoff[h]);
-                sv[h][0] = *reinterpret_cast<const f32x4 *>(sc + h * T::kPixels + q0);
-                sv[h][1] = *reinterpret_cast<const f32x4 *>(sc + h * T::kPixels + q0 + 4);
+                sv[h] = *reinterpret_cast<const u32x4 *>(sc + h * T::kPixels + q0);
             }
 #pragma unroll
             for (int f = 0; f < F; ++f)
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
         auto pair = [&](int p, int to) {                         // of eight: values 2 (p % 4) and the next of piece p / 4
             const int h = p >> 2, e = p & 3;
             float x[2];
-            packed::decode2<FMT>((uint32_t)(e & 2 ? raw[h].y : raw[h].x), e & 1, sv[h][e >> 1][2 * (e & 1)], sv[h][e >> 1][2 * (e & 1) + 1], x);
+            packed::decode2<FMT>((uint32_t)(e & 2 ? raw[h].y : raw[h].x), e & 1, __uint_as_float(sv[h][e] << 16), __uint_as_float(sv[h][e] & 0xFFFF0000u), x);
             bf[to][h][e] = rows::pack2(x[0], x[1]);
         };
         read(0, 0);
@@ -244,6 +244,8 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
                 }
             }
         }
+        // behind the last slice: of a buffer that nothing reads any more
+        scales(slice_of(t + 1), next, made + ((t + 1) & 1) * (T::kMade / 2));
         buf = next;
     }
 
