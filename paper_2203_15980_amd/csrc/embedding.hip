@@ -8,12 +8,14 @@
 // of gw (4 V C bytes) beside one read of gy.
 //   * sort, and zeros beside it: gw is filled with zeros by the launches that sort, whose few workgroups leave the memory idle; rows of ids that occur are
 //     written once more (never more than there are tokens).  Up to kInLds tokens one workgroup sorts (id, position) pairs in LDS; beyond, a stable
-//     radix sort of two digits over all workgroups: each ranks kSortItems tokens by ballots within a wavefront and finds its bases from all
-//     workgroups' digit counts itself.  (One workgroup for 16384 tokens, or sixteen with an id's low bits each, took 23 us where the four launches take 20.)
-//   * sums: a workgroup owns a chunk of sorted places, whose rows of gy it fetches 16 (fp32: 8) at a time, and adds up run by run.  A run of one id
+//     radix sort of two digits over all workgroups: each ranks 256 tokens and more by ballots within a wavefront and finds its bases from all
+//     workgroups' digit counts itself.  (One workgroup for 16384 tokens, or sixteen with an id's low bits each, took 23 us where the four launches took 20.)
+//   * sums: a workgroup owns a chunk of sorted places, whose rows of gy it fetches 8 at a time, and adds up run by run.  A run of one id
 //     that begins and ends in the chunk is a row of gw; what a chunk holds of a run that goes on beyond it becomes a partial sum: its first run in slot 0
 //     if it came in from the chunk before, its last in slot 1 if it began here.  However often an id occurs, a chain is a chunk long.
 //   * joins: the chunk in which a run of several chunks begins adds its slot 1 and the following chunks' slots 0 up to the run's end, a row of gw.
+// us for V = 30522, C = 768, bf16, 16384 tokens: lookup 12.5 (50 MB, 4 TB/s), sort with zeros 28 (94 MB written, 3.4 TB/s), sums 12, joins 4.5; V = 131072,
+// C = 2048, 32768 tokens: 180 (1.07 GB, 6.0 TB/s), 62, 6.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -26,8 +28,13 @@ namespace emb {
 using rows::f32x4;
 
 constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup, chunks of the joins
-constexpr uint32_t kInLds = 1024;                        // most tokens that one workgroup sorts in LDS
-constexpr uint32_t kSortItems = 1024;                    // of a workgroup in the sort over all: 4 wavefronts, 4 rounds of 64 each
+constexpr int kPlaces = 8;                               // rows in flight of the sums (4, 8, 16: the same in bf16; fp32, 16384 x 768: 73, 73, 87 us)
+// Most tokens that one workgroup sorts in LDS: an item is an id and its place in 32 bits.  768 channels, 1024 tokens 28 us, through the four launches 38.
+constexpr uint32_t kInLds = 1024;
+// Sort over all: a workgroup takes 256 tokens up to the first, 512 up to the second, beyond 2048, as every workgroup reads the counts of all.  The whole gradient, us, by
+// 256 / 512 / 2048: of 768 channels, 4096 tokens 33 / 40 / -, 16384 (and the lookup) 57 / 58 / -; of 64 channels, 16384 tokens 27 / 27 / 39, 32768 36 / 34 / 43,
+// 65536 46 / 39 / 46, 131072 69 / 53 / 49, 2097152 - / 1688 / 321.
+constexpr uint32_t kOneRound = 16384, kTwoRounds = 65536;
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
 constexpr long long kMostTokens = 1 << 24;
 
@@ -89,7 +96,7 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
 struct Plan {
     uint32_t n, V, C;
     uint32_t bits, bits1, bits2;                         // of a key and its two digits; an id of no token sorts as V, behind all others
-    uint32_t blocks, chunk, chunks;
+    uint32_t rounds, blocks, chunk, chunks;
     uint64_t key1, pos1, key2, pos2, hist1, hist2, sums, bytes;                    // workspace: byte offsets and size
 };
 
@@ -100,7 +107,9 @@ Plan plan_for(long long n, int V, int C) {
     while ((1u << p.bits) <= (uint32_t)V) ++p.bits;
     p.bits1 = (p.bits + 1) / 2;
     p.bits2 = p.bits - p.bits1;
-    p.blocks = (p.n + kSortItems - 1) / kSortItems;
+    p.rounds = p.n <= kOneRound ? 1 : p.n <= kTwoRounds ? 2 : 8;
+    p.blocks = (p.n + p.rounds * 256 - 1) / (p.rounds * 256);
+    // 16 / 32 / 64 places: 1024 tokens of 768 channels 28 / 32 / 41 us, 4096 38 / 42 / 51, 16384 58 / 60 / 65; 32768 75.5 / 74.5 / 77.6, of 2048 channels 271 / 266 / 269
     p.chunk = p.n <= 16384 ? 16 : 32;
     p.chunks = (p.n + p.chunk - 1) / p.chunk;
     uint64_t at = 0;
@@ -121,7 +130,7 @@ struct Args {
     float *gw;
     uint32_t *key1, *pos1, *key2, *pos2, *hist1, *hist2;
     float *sums;                                         // [chunks][2][C]
-    uint32_t n, V, C, bits, bits1, bits2, blocks, chunk, chunks, pieces;
+    uint32_t n, V, C, bits, bits1, bits2, rounds, blocks, chunk, chunks, pieces;
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t id, uint32_t V) { return (uint64_t)id < V ? (uint32_t)id : V; }
@@ -230,19 +239,19 @@ __global__ __launch_bounds__(256) void sort_kernel(Args a) {
 }
 
 // Digit counts of a pass, [block][digit]; the workgroups behind fill gw.
-template <bool FIRST>
+template <bool FIRST, int ROUNDS>
 __global__ __launch_bounds__(256) void count_kernel(Args a) {
     if (blockIdx.x >= a.blocks) {
         fill(a, a.blocks, FIRST ? 0 : 4, FIRST ? 1 : 5);           // counting is over in half a scatter's time
         return;
     }
     __shared__ uint32_t bins[kMostBins];
-    const uint32_t nbins = 1u << (FIRST ? a.bits1 : a.bits2), i0 = blockIdx.x * kSortItems;
+    const uint32_t nbins = 1u << (FIRST ? a.bits1 : a.bits2), i0 = blockIdx.x * (ROUNDS * 256);
     uint32_t *hist = (FIRST ? a.hist1 : a.hist2) + (uint64_t)blockIdx.x * nbins;
     for (uint32_t i = threadIdx.x; i < nbins; i += 256) bins[i] = 0;
     __syncthreads();
 #pragma unroll
-    for (uint32_t r = 0; r < kSortItems / 256; ++r) {
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
         const uint32_t i = i0 + r * 256 + threadIdx.x;
         if (i < a.n) atomicAdd(&bins[FIRST ? key_of(a.id[i], a.V) & (nbins - 1) : a.key1[i] >> a.bits1], 1u);
     }
@@ -251,7 +260,7 @@ __global__ __launch_bounds__(256) void count_kernel(Args a) {
 }
 
 // One pass of the sort: each token to its place by the digit, in the order the tokens come in.
-template <bool FIRST>
+template <bool FIRST, int ROUNDS>
 __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     if (blockIdx.x >= a.blocks) {
         fill(a, a.blocks, FIRST ? 1 : 5, FIRST ? 4 : 8);
@@ -260,14 +269,13 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     __shared__ uint32_t base[kMostBins];                 // where this workgroup's tokens of a digit begin
     __shared__ uint32_t mine[4][kMostBins];              // tokens of a digit in each wavefront; then in those before it
     __shared__ uint32_t part[4];
-    constexpr int kRounds = kSortItems / 256;
     const uint32_t bits = FIRST ? a.bits1 : a.bits2, shift = FIRST ? 0 : a.bits1, nbins = 1u << bits;
     const uint32_t *hist = FIRST ? a.hist1 : a.hist2;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t i0 = blockIdx.x * kSortItems + wave * (kSortItems / 4);
-    uint32_t key[kRounds], pos[kRounds], rank[kRounds];
+    const uint32_t i0 = (blockIdx.x * 4 + wave) * (ROUNDS * 64);
+    uint32_t key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const uint32_t i = i0 + r * 64 + lane;
         key[r] = 0; pos[r] = i;
         if (i >= a.n) continue;
@@ -302,7 +310,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     }
     // ranks within a wavefront: how many lanes before hold the same digit, after the rounds before (`mine` is cleared: sum_before has a barrier)
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const bool live = i0 + r * 64 + lane < a.n;
         const uint32_t d = (key[r] >> shift) & (nbins - 1);
         const uint64_t same = same_digit(d, bits, live);
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         if (i0 + r * 64 + lane >= a.n) continue;
         const uint32_t to = mine[wave][(key[r] >> shift) & (nbins - 1)] + rank[r];
         if (FIRST) {
@@ -344,8 +352,8 @@ __device__ __forceinline__ void put(float *out, const float (&v)[8]) {
     reinterpret_cast<f32x4 *>(out)[1] = f32x4{v[4], v[5], v[6], v[7]};
 }
 
-// A workgroup's chunk of sorted places, run by run, PLACES rows in flight.
-template <typename T, int PLACES>
+// A workgroup's chunk of sorted places, run by run, kPlaces rows in flight.
+template <typename T>
 __global__ __launch_bounds__(1024) void sums_kernel(Args a) {
     const uint32_t piece = threadIdx.x, lane = piece & 63, from = blockIdx.x * a.chunk, size = from + a.chunk < a.n ? a.chunk : a.n - from;
     const uint32_t mine = from + (lane < size ? lane : size - 1);                  // a lane to a place: chunks have at most 64
@@ -368,16 +376,16 @@ __global__ __launch_bounds__(1024) void sums_kernel(Args a) {
             put(a.gw + (uint64_t)run * a.C + piece * 8, sum);
         }
     };
-    for (uint32_t i = 0; i < size; i += PLACES) {
-        rows::Eight<T> raw[PLACES];
+    for (uint32_t i = 0; i < size; i += kPlaces) {
+        rows::Eight<T> raw[kPlaces];
 #pragma unroll
-        for (int k = 0; k < PLACES; ++k) {
+        for (int k = 0; k < kPlaces; ++k) {
             const uint32_t m = (uint32_t)__builtin_amdgcn_readlane((int)places, (int)(i + k));         // behind the chunk: its last place
             raw[k].zero();
             if (live && (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)(i + k)) < a.V) raw[k].load(a.gy + (uint64_t)m * a.C * sizeof(T) + piece * 8 * sizeof(T));
         }
 #pragma unroll
-        for (int k = 0; k < PLACES; ++k) {
+        for (int k = 0; k < kPlaces; ++k) {
             if (i + k >= size) break;
             const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)(i + k));
             if (key != run) {
@@ -473,10 +481,20 @@ hipError_t launch_embedding(const void *id, const void *w, const float *scale, v
 
 size_t embedding_bwd_workspace_bytes(long long n, int V, int C) { return emb::plan_for(n, V, C).bytes; }
 
-// Workgroups that fill gw beside a sort: enough to keep the memory busy, no more than there is work for.
+// Workgroups that fill gw beside a sort: no more than there is work for, and three to a compute unit.  512 / 768 / 1024 / 2048 for V = 131072, C = 2048: 260 / 248 /
+// 264 / 271 us; for V = 30522, C = 768: 58 / 57 / 58 / 57.
 static uint32_t fillers(const emb::Args &a, uint32_t eighths) {
-    const uint64_t want = (uint64_t)a.V * a.C / 4 * eighths / 8 / (256 * 4) + 1, most = 2048;
+    const uint64_t want = (uint64_t)a.V * a.C / 4 * eighths / 8 / (256 * 4) + 1, most = 768;
     return (uint32_t)(want < most ? want : most);
+}
+
+template <int ROUNDS>
+static void sort(const emb::Args &a, hipStream_t stream) {
+    const dim3 counting(a.blocks + fillers(a, 1)), scattering(a.blocks + fillers(a, 3)), block(256);
+    emb::count_kernel<true, ROUNDS><<<counting, block, 0, stream>>>(a);
+    emb::scatter_kernel<true, ROUNDS><<<scattering, block, 0, stream>>>(a);
+    emb::count_kernel<false, ROUNDS><<<counting, block, 0, stream>>>(a);
+    emb::scatter_kernel<false, ROUNDS><<<scattering, block, 0, stream>>>(a);
 }
 
 template <typename T>
@@ -484,15 +502,15 @@ static hipError_t embedding_bwd(const emb::Args &a, hipStream_t stream) {
     using namespace emb;
     if (a.n <= kInLds) {
         sort_kernel<<<dim3(1 + fillers(a, 8)), dim3(256), 0, stream>>>(a);
+    } else if (a.rounds == 1) {
+        sort<1>(a, stream);
+    } else if (a.rounds == 2) {
+        sort<2>(a, stream);
     } else {
-        const dim3 counting(a.blocks + fillers(a, 1)), scattering(a.blocks + fillers(a, 3)), block(256);
-        count_kernel<true><<<counting, block, 0, stream>>>(a);
-        scatter_kernel<true><<<scattering, block, 0, stream>>>(a);
-        count_kernel<false><<<counting, block, 0, stream>>>(a);
-        scatter_kernel<false><<<scattering, block, 0, stream>>>(a);
+        sort<8>(a, stream);
     }
     const uint32_t threads = (a.pieces + 63) / 64 * 64;
-    sums_kernel<T, sizeof(T) == 2 ? 16 : 8><<<dim3(a.chunks), dim3(threads), 0, stream>>>(a);
+    sums_kernel<T><<<dim3(a.chunks), dim3(threads), 0, stream>>>(a);
     if (a.chunks > 1) {
         const uint32_t side = a.pieces >= 256 ? 1 : 512 / a.pieces < 8 ? 512 / a.pieces : 8;
         joins_kernel<<<dim3(a.chunks - 1), dim3((a.pieces * side + 63) / 64 * 64), side * a.C * sizeof(float), stream>>>(a, side);
@@ -513,7 +531,7 @@ hipError_t launch_embedding_bwd(const void *id, const void *gy, const float *sca
     a.key1 = u32(p.key1); a.pos1 = u32(p.pos1); a.key2 = u32(p.key2); a.pos2 = u32(p.pos2);
     a.hist1 = u32(p.hist1); a.hist2 = u32(p.hist2);
     a.sums = reinterpret_cast<float *>(ws + p.sums);
-    a.n = p.n; a.V = p.V; a.C = p.C; a.bits = p.bits; a.bits1 = p.bits1; a.bits2 = p.bits2; a.blocks = p.blocks;
+    a.n = p.n; a.V = p.V; a.C = p.C; a.bits = p.bits; a.bits1 = p.bits1; a.bits2 = p.bits2; a.rounds = p.rounds; a.blocks = p.blocks;
     a.chunk = p.chunk; a.chunks = p.chunks; a.pieces = (uint32_t)C / 8;
     return bf16 ? embedding_bwd<rows::bf16>(a, stream) : embedding_bwd<float>(a, stream);
 }

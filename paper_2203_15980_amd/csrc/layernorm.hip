@@ -5,11 +5,13 @@
 // mean and var come from x again: the row is read anyway, and nothing but x has to be kept (DELTA's Assumptions 1-3: the backward pass reads stored
 // forward activations).  x may be a checkpoint in 8 bits (packed.hpp), read as it lies.
 //
-// Bound by memory, 3 reads or writes of the tensor for the gradients (6 bytes a value in bf16, 5.03 with x in 8 bits) and 2 forward.  Up to 2048 channels (backward:
-// 1024) a wavefront owns a row and keeps it in registers; beyond, a workgroup does, eight channels a thread.  Workers are persistent over rows, the next
+// Bound by memory, 3 reads or writes of the tensor for the gradients (6 bytes a value in bf16, 5.03 with x in 8 bits) and 2 forward.  Up to 2048 channels a wavefront owns a row and
+// keeps it in registers (backward: of few rows up to 1024); beyond, a workgroup does, eight channels a thread.  Workers are persistent over rows, the next
 // row's loads in flight while one is worked on, and keep their sums of dgamma and dbeta in registers: a workgroup writes one partial sum of 2 C values and
 // a second kernel adds those in a fixed order (no atomics: a fixed function of the inputs).  All statistics and sums are fp32: the mean first,
 // then the variance of the centred values.
+// us, and the second kernel's beside them, with 16384 rows of 768 channels: bf16 17 + 4 (75 MB, 4.4 TB/s; from int8 17 + 4), fp32 27 + 5 (151 MB, 5.6 TB/s), forward
+// 21 (100 MB, 4.8 TB/s); 8192 rows of 8192 channels with gx_add, bf16 108 + 7 (537 MB, 5.0 TB/s), forward 61 (268 MB, 4.4 TB/s); 77 rows of 768 4.6 + 2.3.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -24,7 +26,10 @@ using packed::u32x2;
 using rows::f32x4;
 
 constexpr int kRowChannels = 2048, kMostChannels = 8192; // forward: a wavefront owns a row up to the first
-constexpr int kWaveChannels = 1024;                      // backward: a wavefront owns a row up to here
+// Backward: whether a wavefront owns a row.  Up to 1024 channels always; up to 2048 if there are rows enough for 128 workgroups of them.  Both kernels, us, a
+// wavefront's first: 768 channels, 16384 rows 22 and 46; 1536 channels, 8192 rows 21 and 30; 2048 channels, 8192 rows 25 and 34; 1536 channels, 2048
+// rows 24 and 24, 77 rows 8.1 and 6.4; 2048 channels, 200 rows 13.4 and 12.8.
+constexpr bool row_to_wave(long long rows, int C) { return C <= 1024 || (C <= 2048 && rows >= 1024); }
 // Wavefronts of its workgroup.  The same for a tensor and its checkpoint, with and without gx_add: the sums' order, and so their bits, do not depend on those.
 template <int R> constexpr int kWaves = R == 1 ? 16 : 8;
 
@@ -317,9 +322,12 @@ __global__ __launch_bounds__(1024) void partials_kernel(const float *partial, fl
     out[c] = s;
 }
 
-// Workgroups of the backward launch: as many as are resident at once, and no more than there are rows for.
+// Workgroups of the backward launch: no more than there are rows for, and at most those that measured best, of 128, 256, 512 and 1024, us:
+// 512 channels 20, 16, 18, -; 768 channels 30, 20.1, 20.9, -; 1536 channels -, 21, 25, -; 2048 channels, a wavefront's, -, 25, 32, -;
+// 4096 channels (to a workgroup, forward too) -, 96, 89, 102; 8192 channels 245, 178, 192, -.
 uint32_t workgroups(long long rows, int C) {
-    const long long per = C <= 512 ? kWaves<1> : C <= kWaveChannels ? kWaves<2> : 1, most = C <= kWaveChannels ? 256 : C <= 4096 ? 512 : 256;
+    const bool wave = row_to_wave(rows, C);
+    const long long per = !wave ? 1 : C <= 512 ? kWaves<1> : kWaves<2>, most = !wave && C <= 4096 ? 512 : 256;
     const long long want = (rows + per - 1) / per;
     return (uint32_t)(want < most ? want : most);
 }
@@ -354,16 +362,18 @@ size_t layernorm_bwd_workspace_bytes(long long rows, int C) { return (size_t)ln:
 
 template <typename T, int FMT, bool ADD>
 static hipError_t layernorm_bwd(const ln::Args &a, uint32_t grid, hipStream_t stream) {
-    if (a.C > ln::kWaveChannels) {
+    if (!ln::row_to_wave(a.rows, (int)a.C)) {
         ln::backward_wide_kernel<T, FMT, ADD><<<dim3(grid), dim3((a.C / 8 + 63) / 64 * 64), 0, stream>>>(a);
         return hipGetLastError();
     }
     auto run = [&](auto kernel, unsigned waves) {
         const size_t sums = a.partial ? (size_t)waves * a.C : 0, gamma = (a.C + 511) / 512 * 512;
-        kernel<<<dim3(grid), dim3(waves * 64), (sums > gamma ? sums : gamma) * sizeof(float), stream>>>(a);              // 32 KB at most
+        kernel<<<dim3(grid), dim3(waves * 64), (sums > gamma ? sums : gamma) * sizeof(float), stream>>>(a);              // 64 KB at most
     };
     if (a.C <= 512) run(ln::backward_kernel<T, FMT, ADD, 1>, ln::kWaves<1>);
-    else run(ln::backward_kernel<T, FMT, ADD, 2>, ln::kWaves<2>);
+    else if (a.C <= 1024) run(ln::backward_kernel<T, FMT, ADD, 2>, ln::kWaves<2>);
+    else if (a.C <= 1536) run(ln::backward_kernel<T, FMT, ADD, 3>, ln::kWaves<3>);
+    else run(ln::backward_kernel<T, FMT, ADD, 4>, ln::kWaves<4>);
     return hipGetLastError();
 }
 template <typename T>
