@@ -1350,7 +1350,7 @@ BwdKind bwd_kind(const delta_layer_desc &L) {
     if (L.op == DELTA_OP_LAYERNORM) return BK_LAYERNORM;
     if (L.op == DELTA_OP_EMBEDDING) return BK_EMBEDDING;
     if (is_stem(L)) return BK_STEM;
-    if (L.H == 1 && L.W == 1 && L.R == 1 && L.S == 1 && L.stride == 1 && L.pad == 0 && L.Cout % 64 != 0) return BK_DENSE;
+    if (L.op == DELTA_OP_CONV && L.H == 1 && L.W == 1 && L.R == 1 && L.S == 1 && L.stride == 1 && L.pad == 0 && L.Cout % 64 != 0) return BK_DENSE;
     return BK_CONV;
 }
 
@@ -1515,8 +1515,8 @@ bool wgrad_aside(const delta_layer_desc &L, const delta::ConvArgs &fa) {
     const uint64_t rows = L.stride == 2 && L.R == 3 ? (uint64_t)fa.M / 4 : (uint64_t)fa.M;
     return 2ull * rows * fa.R * fa.S * fa.Cin * fa.Cout >= kAsideFlops;
 }
-// From a checkpoint and without a data gradient beside it the weight gradient stays on the compute stream at any size: 768 -> 768 on 16384 tokens 48 us, 62 with
-// the events of the other stream.
+// From a checkpoint and without a data gradient beside it the weight gradient stays on the compute stream at any size: on 16384 tokens 768 -> 768 38 us a call,
+// 60 with the events of the other stream, 2048 -> 2048 190 and 209.
 bool goes_aside(const delta_bwd_desc &D, const delta::ConvArgs &fa) {
     return wgrad_aside(D.fwd, fa) && !(D.fwd.pack && D.gx == DELTA_NO_TENSOR);
 }

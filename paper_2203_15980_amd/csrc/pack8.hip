@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(Args a) {
 
 const char *pack8_check(const void *x, const void *y, long long rows, int C, int fmt) {
     if (fmt != PACK_INT8 && fmt != PACK_E4M3) return "a checkpoint is DELTA_PACK_INT8 or DELTA_PACK_E4M3";
-    if (rows <= 0 || C <= 0 || C % 8) return "channels must be a multiple of 8";
+    if (rows <= 0 || rows > 0x7FFFFFFFLL || C <= 0 || C % 8) return "channels must be a multiple of 8";
     if (rows * ((C + kPackBlock - 1LL) / kPackBlock) > 0x7FFFFFFFLL / 4) return "too many rows for a checkpoint";
     if (!x || !y || (((uintptr_t)x | (uintptr_t)y) & 15)) return "pointers must be non-null and 16-byte aligned";
     return nullptr;

@@ -95,7 +95,7 @@ def test_the_checkpoint_of_what_a_checkpoint_holds_is_the_same(torch_mod):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("rows,C,dtype", [(1, 8, "bf16"), (77, 768, "bf16"), (9, 1000, "bf16"), (33, 520, "f32"), (5, 1032, "bf16"), (3, 8192, "bf16"),
-                                          (17, 2112, "f32"), (4500, 96, "bf16")])
+                                          (17, 2112, "f32"), (4500, 96, "bf16"), (1029, 1544, "bf16"), (1024, 2048, "f32"), (1023, 2048, "bf16")])
 def test_layernorm_gradients_from_a_checkpoint(torch_mod, rows, C, dtype, fmt):
     print("rows", rows, "C", C, dtype, fmt, flush=True)
     rng = np.random.default_rng(rows + C)
@@ -256,4 +256,25 @@ def test_refusals(torch_mod):
     refused(bw, b.bwd(fwd, 3, gw=gw))
     refused(bw, b.bwd(b.layer(dl.OP_RELU, rows, C, C, 1, 2, pack=1), 3, gx=4))
     refused(bw, b.bwd(b.layer(dl.OP_CONV, rows // 4, C, C, 1, 2, pack=1, W=4, R=3, S=3, pad=1, **lin), 3, gw=gw, ws=ws))
+    b.close()
+
+
+@pytest.mark.parametrize("shape", [dict(N=16, H=1), dict(N=1, H=16)])
+def test_making_and_restoring_a_checkpoint_have_no_backward(torch_mod, shape):
+    """Neither is taken for the classifier, whose layers are [N, 1, 1] too and which reads weights that these have not."""
+    rows, C = 16, 8
+    nb, pb = rows * C * 2, ro.packed_bytes(rows, C)
+    b = Bench(torch_mod, [nb, pb, nb, nb, pb, nb])
+    dl = b.dl
+    gw, _ = b.guarded(C * C)
+    ws, _ = b.workspace(4096)
+    for i in (0, 1, 2, 4):
+        b.put(i, np.zeros((nb, pb, nb, nb, pb)[i], np.uint8))
+    for op, x, y, gy, gx in ((dl.OP_PACK8, 0, 1, 4, 3), (dl.OP_UNPACK8, 1, 2, 0, 4)):
+        fwd = b.layer(op, rows, C, C, x, y, pack=dl.PACK_INT8, **shape)
+        for desc in (b.bwd(fwd, gy, gx=gx), b.bwd(fwd, gy, gw=gw, ws=ws), b.bwd(fwd, gy, gx=gx, gw=gw, ws=ws)):
+            for call in (lambda: b.d.backward_segment([desc]), lambda: b.d.backward_kernel(desc)):
+                with pytest.raises(dl.DeltaError) as e:
+                    call()
+                assert e.value.status == dl.ERR_INVALID, e.value.message
     b.close()

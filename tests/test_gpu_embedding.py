@@ -39,7 +39,8 @@ GRADIENT = [(1, 1, 8, "any"), (1, 100, 768, "any"), (63, 7, 64, "any"), (64, 2, 
             (4096, 257, 64, "bad"), (5000, 4, 520, "runs"), (5000, 30522, 768, "falling"), (9000, 50, 64, "none"), (16384, 30522, 96, "falling"),
             (16384, 100, 64, "same"), (20000, 2 ** 17, 8, "any"), (40001, 1000, 16, "falling"), (70000, 2 ** 22 - 1, 8, "bad"), (300, 2 ** 22 - 1, 8, "any"),
             (2100, 33, 8192, "runs"), (1024, 300, 64, "falling"), (1025, 300, 64, "falling"), (4096, 2 ** 18, 8, "any"), (4097, 2 ** 18 - 1, 8, "falling"),
-            (16384, 2 ** 20, 8, "bad"), (16385, 3, 64, "same"), (16401, 7, 64, "runs"), (33, 7, 64, "same"), (48, 3, 64, "runs"), (65537, 3, 8, "same")]
+            (16384, 2 ** 20, 8, "bad"), (16385, 3, 64, "same"), (16401, 7, 64, "runs"), (33, 7, 64, "same"), (48, 3, 64, "runs"), (65537, 3, 8, "same"),
+            (16383, 300, 16, "falling"), (65536, 100, 8, "falling"), (65537, 2 ** 17, 16, "bad"), (200001, 3000, 8, "falling")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -30,7 +30,8 @@ def _case(rows, C, dtype, seed=0, shift=1.5):
 
 # rows: one, fewer than a workgroup has wavefronts, ragged, more than one round of the persistent workers
 SHAPES = [(1, 8), (1, 768), (3, 64), (7, 512), (9, 520), (77, 768), (8, 1024), (65, 1032), (130, 2048), (5, 2112), (33, 4096), (3, 8192),
-          (4500, 64), (4099, 768), (600, 2560), (1100, 1536)]
+          (4500, 64), (4099, 768), (600, 2560), (1100, 1536),
+          (1023, 1544), (1024, 1544), (1025, 2048), (2050, 1032), (1030, 2112)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
