@@ -7,14 +7,14 @@
 // Gradient: rows of gw from the tokens in sorted order; no atomics on values, so the sums' order is fixed by the ids alone.  What bounds it is the write
 // of gw (4 V C bytes) beside one read of gy.
 //   * sort, and zeros beside it: gw is filled with zeros by the launches that sort, whose few workgroups leave the memory idle; rows of ids that occur are
-//     written once more (never more than there are tokens).  Up to kInLds tokens one workgroup sorts (id, position) pairs in LDS; beyond, a stable
+//     written once more (never more than there are tokens).  Up to 8192 tokens one workgroup sorts (id, position) pairs in LDS; beyond, a stable
 //     radix sort of two digits over all workgroups: each ranks 256 tokens and more by ballots within a wavefront and finds its bases from all
 //     workgroups' digit counts itself.  (One workgroup for 16384 tokens, or sixteen with an id's low bits each, took 23 us where the four launches took 20.)
 //   * sums: a workgroup owns a chunk of sorted places, whose rows of gy it fetches 8 at a time, and adds up run by run.  A run of one id
 //     that begins and ends in the chunk is a row of gw; what a chunk holds of a run that goes on beyond it becomes a partial sum: its first run in slot 0
 //     if it came in from the chunk before, its last in slot 1 if it began here.  However often an id occurs, a chain is a chunk long.
 //   * joins: the chunk in which a run of several chunks begins adds its slot 1 and the following chunks' slots 0 up to the run's end, a row of gw.
-// us for V = 30522, C = 768, bf16, 16384 tokens: lookup 12.5 (50 MB, 4 TB/s), sort with zeros 28 (94 MB written, 3.4 TB/s), sums 12, joins 4.5; V = 131072,
+// us for V = 30522, C = 768, bf16, 16384 tokens: lookup 13 (50 MB, 4 TB/s), sort with zeros 28 (94 MB written, 3.4 TB/s), sums 12, joins 4.5; V = 131072,
 // C = 2048, 32768 tokens: 180 (1.07 GB, 6.0 TB/s), 62, 6.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -30,10 +30,11 @@ using rows::f32x4;
 constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup, chunks of the joins
 constexpr uint32_t kCounts = 16;                         // workgroups' counts of a digit in flight (8, 16, 32: 16384 tokens 45, 43, 42 us; 40000 119, 116, 117)
 constexpr int kPlaces = 8;                               // rows in flight of the sums (4, 8, 16: the same in bf16; fp32, 16384 x 768: 73, 73, 87 us)
-// Most tokens that one workgroup sorts in LDS: an item is an id and its place in 32 bits.  768 channels, 1024 tokens 28 us, through the four launches 38.
-constexpr uint32_t kInLds = 1024;
+// Tokens that one workgroup sorts in LDS, places for 1024, 4096 or 8192; an item is an id above its place, in 32 bits.  The whole gradient, us, so / through the four
+// launches of the sort over all: 30522 x 768, 1024 tokens 28 / 38, 1100 25 / 33, 4096 26 / 34, 8192 32 / 39; 30522 x 64, 2048 21 / 23, 6000 26 / 25.
+constexpr uint32_t places_in_lds(uint32_t n, uint32_t bits) { return n <= 1024 ? 1024 : n <= 4096 && bits <= 20 ? 4096 : n <= 8192 && bits <= 19 ? 8192 : 0; }
 // Sort over all: a workgroup takes 256 tokens up to the first, 512 up to the second, beyond 2048, as every workgroup reads the counts of all.  The whole gradient, us, by
-// 256 / 512 / 2048: of 768 channels, 4096 tokens 33 / 40 / -, 16384 (and the lookup) 57 / 58 / -; of 64 channels, 16384 tokens 27 / 27 / 39, 32768 36 / 34 / 43,
+// 256 / 512 / 2048: of 768 channels, 16384 tokens (and the lookup) 57 / 58 / -; of 64 channels, 16384 tokens 27 / 27 / 39, 32768 36 / 34 / 43,
 // 65536 46 / 39 / 46, 131072 69 / 53 / 49, 2097152 - / 1688 / 321.
 constexpr uint32_t kOneRound = 16384, kTwoRounds = 65536;
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
@@ -95,6 +96,7 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
 
 // ---- gradient
 struct Plan {
+    uint32_t in_lds;                                     // places of the sort in one workgroup, or 0: over all
     uint32_t n, V, C;
     uint32_t bits, bits1, bits2;                         // of a key and its two digits; an id of no token sorts as V, behind all others
     uint32_t rounds, blocks, chunk, chunks;
@@ -115,10 +117,10 @@ Plan plan_for(long long n, int V, int C) {
     p.chunks = (p.n + p.chunk - 1) / p.chunk;
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const bool one = p.n <= kInLds;
-    p.key1 = take(one ? 0 : 4ull * p.n); p.pos1 = take(one ? 0 : 4ull * p.n);
+    p.in_lds = places_in_lds(p.n, p.bits);
+    p.key1 = take(p.in_lds ? 0 : 4ull * p.n); p.pos1 = take(p.in_lds ? 0 : 4ull * p.n);
     p.key2 = take(4ull * p.n); p.pos2 = take(4ull * p.n);
-    p.hist1 = take(one ? 0 : (4ull << p.bits1) * p.blocks); p.hist2 = take(one ? 0 : (4ull << p.bits2) * p.blocks);
+    p.hist1 = take(p.in_lds ? 0 : (4ull << p.bits1) * p.blocks); p.hist2 = take(p.in_lds ? 0 : (4ull << p.bits2) * p.blocks);
     p.sums = take(8ull * p.chunks * p.C);
     p.bytes = at;
     return p;
@@ -131,7 +133,7 @@ struct Args {
     float *gw;
     uint32_t *key1, *pos1, *key2, *pos2, *hist1, *hist2;
     float *sums;                                         // [chunks][2][C]
-    uint32_t n, V, C, bits, bits1, bits2, rounds, blocks, chunk, chunks, pieces;
+    uint32_t n, V, C, bits, bits1, bits2, in_lds, rounds, blocks, chunk, chunks, pieces;
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t id, uint32_t V) { return (uint64_t)id < V ? (uint32_t)id : V; }
@@ -154,15 +156,16 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, uint32_t bits, bool l
     return same;
 }
 
-// LDS of the sort in one workgroup: four neighbouring items to a thread.  Every 16th word is followed by an unused one: a thread's words lie side by side.
-struct SortLds {
-    uint32_t item[kInLds * 17 / 16];
-    uint32_t count[256 * 16 * 17 / 16];                  // two counts to a word, [digit][thread]
-    uint32_t part[4];
+// LDS of the sort in one workgroup: neighbouring items to a thread.  Every 16th word is followed by an unused one: a thread's words lie side by side.
+template <int THREADS, int ITEMS, int WIDTH> struct SortLds {
+    uint32_t item[(uint32_t)ITEMS * THREADS * 17 / 16];
+    uint32_t count[(1 << WIDTH) * THREADS / 2 * 17 / 16];          // two counts to a word, [digit][thread]
+    uint32_t part[THREADS / 64];
 };
 __device__ __forceinline__ uint32_t spaced(uint32_t i) { return i + (i >> 4); }
 
-// The sum of v over the 256 threads' before this one; `part`: a word to a wavefront.
+// The sum of v over the threads before this one; `part`: a word to a wavefront.
+template <int THREADS>
 __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *part) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t run = v;
@@ -175,53 +178,54 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *part) {
     __syncthreads();
     run -= v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) run += (uint32_t)i < wave ? part[i] : 0;
+    for (int i = 0; i < THREADS / 64; ++i) run += (uint32_t)i < wave ? part[i] : 0;
     return run;
 }
 
-// Workgroup 0 sorts all tokens, the others fill gw.  An item is an id above its position, in 32 bits.  A pass (at most 5 bits) counts each thread's digits in a
-// column of its own, sums the counts by (digit, thread), which is the sorted order of equal digits, and moves each item to its count's sum.
-__global__ __launch_bounds__(256) void sort_kernel(Args a) {
-    constexpr uint32_t kPlaceBits = 10, kItems = 4;
-    static_assert(kInLds == 1u << kPlaceBits && kInLds == kItems * 256 && kPlaceBits + kMostBits <= 32, "an item is 32 bits");
+// Workgroup 0 sorts all tokens, the others fill gw.  An item is an id above its position, in 32 bits.  A pass (at most WIDTH bits) counts each thread's digits
+// in a column of its own, sums the counts by (digit, thread), which is the sorted order of equal digits, and moves each item to its count's sum.
+template <int THREADS, int ITEMS, int WIDTH>
+__global__ __launch_bounds__(THREADS) void sort_kernel(Args a) {
+    constexpr uint32_t kMost = (uint32_t)ITEMS * THREADS, kPlaceBits = kMost == 1024 ? 10 : kMost == 4096 ? 12 : 13;
+    static_assert(kMost == 1u << kPlaceBits, "an item is 32 bits");
     if (blockIdx.x) {
         fill(a, 1, 0, 8);
         return;
     }
-    __shared__ SortLds l;
+    __shared__ SortLds<THREADS, ITEMS, WIDTH> l;
     uint16_t *const count = reinterpret_cast<uint16_t *>(l.count);
     const uint32_t tid = threadIdx.x;
 #pragma unroll
-    for (uint32_t k = 0; k < kItems; ++k) {              // what is behind the last token sorts behind it: all its bits are set, and it comes last
-        const uint32_t i = tid + k * 256;
+    for (uint32_t k = 0; k < (uint32_t)ITEMS; ++k) {          // what is behind the last token sorts behind it: all its bits are set, and it comes last
+        const uint32_t i = tid + k * THREADS;
         l.item[spaced(i)] = i < a.n ? key_of(a.id[i], a.V) << kPlaceBits | i : ~0u;
     }
-    const uint32_t passes = (a.bits + 4) / 5, width = (a.bits + passes - 1) / passes, words = (1u << width) / 2;     // words of counts a thread sums
+    const uint32_t passes = (a.bits + WIDTH - 1) / WIDTH, width = (a.bits + passes - 1) / passes, words = (1u << width) / 2;     // words of counts a thread sums
     const uint32_t column = spaced(tid / 2) * 2 + (tid & 1);
-    auto at = [&](uint32_t d) { return d * (256 * 17 / 16) + column; };             // spaced(d * 128 + tid / 2)
+    auto at = [&](uint32_t d) { return d * (THREADS * 17 / 16) + column; };        // spaced(d * THREADS / 2 + tid / 2)
     for (uint32_t p = 0; p < passes; ++p) {
         const uint32_t shift = kPlaceBits + p * width, mask = (1u << width) - 1;
-        for (uint32_t i = tid; i < spaced(words * 256); i += 256) l.count[i] = 0;
+        for (uint32_t i = tid; i < spaced(words * THREADS); i += THREADS) l.count[i] = 0;
         __syncthreads();
-        uint32_t item[kItems], rank[kItems];
+        uint32_t item[(uint32_t)ITEMS], rank[(uint32_t)ITEMS];
 #pragma unroll
-        for (uint32_t k = 0; k < kItems; ++k) item[k] = l.item[spaced(tid * kItems + k)];
+        for (uint32_t k = 0; k < (uint32_t)ITEMS; ++k) item[k] = l.item[spaced(tid * (uint32_t)ITEMS + k)];
 #pragma unroll
-        for (uint32_t k = 0; k < kItems; ++k) {
+        for (uint32_t k = 0; k < (uint32_t)ITEMS; ++k) {
             const uint32_t i = at(item[k] >> shift & mask);
             rank[k] = count[i];
             count[i] = (uint16_t)(rank[k] + 1);
         }
         __syncthreads();
-        uint32_t w[16], sum = 0;
+        uint32_t w[(1 << WIDTH) / 2], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < (1 << WIDTH) / 2; ++j) {
             w[j] = (uint32_t)j < words ? l.count[spaced(tid * words + j)] : 0;
             sum += (w[j] & 0xFFFFu) + (w[j] >> 16);
         }
-        uint32_t run = sum_before(sum, l.part);
+        uint32_t run = sum_before<THREADS>(sum, l.part);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < (1 << WIDTH) / 2; ++j) {
             if ((uint32_t)j >= words) break;
             const uint32_t second = run + (w[j] & 0xFFFFu);
             l.count[spaced(tid * words + j)] = run | second << 16;
@@ -229,13 +233,13 @@ __global__ __launch_bounds__(256) void sort_kernel(Args a) {
         }
         __syncthreads();
 #pragma unroll
-        for (uint32_t k = 0; k < kItems; ++k) l.item[spaced(count[at(item[k] >> shift & mask)] + rank[k])] = item[k];
+        for (uint32_t k = 0; k < (uint32_t)ITEMS; ++k) l.item[spaced(count[at(item[k] >> shift & mask)] + rank[k])] = item[k];
         __syncthreads();
     }
-    for (uint32_t i = tid; i < a.n; i += 256) {
+    for (uint32_t i = tid; i < a.n; i += THREADS) {
         const uint32_t v = l.item[spaced(i)];
         a.key2[i] = v >> kPlaceBits;
-        a.pos2[i] = v & (kInLds - 1);
+        a.pos2[i] = v & (kMost - 1);
     }
 }
 
@@ -313,7 +317,7 @@ __global__ __launch_bounds__(256) void scatter_kernel(Args a) {
         }
         sum += all[k];
     }
-    uint32_t run = sum_before(sum, part);
+    uint32_t run = sum_before<256>(sum, part);
 #pragma unroll
     for (int k = 0; k < kMostBins / 256; ++k) {
         const uint32_t d = tid * per + k;
@@ -496,14 +500,14 @@ size_t embedding_bwd_workspace_bytes(long long n, int V, int C) { return emb::pl
 
 // Workgroups that fill gw beside a sort: no more than there is work for, and three to a compute unit.  512 / 768 / 1024 / 2048 for V = 131072, C = 2048: 260 / 248 /
 // 264 / 271 us; for V = 30522, C = 768: 58 / 57 / 58 / 57.
-static uint32_t fillers(const emb::Args &a, uint32_t eighths) {
-    const uint64_t want = (uint64_t)a.V * a.C / 4 * eighths / 8 / (256 * 4) + 1, most = 768;
+static uint32_t fillers(const emb::Args &a, uint32_t eighths, uint32_t threads) {
+    const uint64_t want = (uint64_t)a.V * a.C / 4 * eighths / 8 / (threads * 4) + 1, most = threads == 256 ? 768 : 256;        // as many threads
     return (uint32_t)(want < most ? want : most);
 }
 
 template <int ROUNDS>
 static void sort(const emb::Args &a, hipStream_t stream) {
-    const dim3 counting(a.blocks + fillers(a, 1)), scattering(a.blocks + fillers(a, 3)), block(256);
+    const dim3 counting(a.blocks + fillers(a, 1, 256)), scattering(a.blocks + fillers(a, 3, 256)), block(256);
     emb::count_kernel<true, ROUNDS><<<counting, block, 0, stream>>>(a);
     emb::scatter_kernel<true, ROUNDS><<<scattering, block, 0, stream>>>(a);
     emb::count_kernel<false, ROUNDS><<<counting, block, 0, stream>>>(a);
@@ -513,8 +517,12 @@ static void sort(const emb::Args &a, hipStream_t stream) {
 template <typename T>
 static hipError_t embedding_bwd(const emb::Args &a, hipStream_t stream) {
     using namespace emb;
-    if (a.n <= kInLds) {
-        sort_kernel<<<dim3(1 + fillers(a, 8)), dim3(256), 0, stream>>>(a);
+    if (a.in_lds == 1024) {
+        sort_kernel<256, 4, 5><<<dim3(1 + fillers(a, 8, 256)), dim3(256), 0, stream>>>(a);
+    } else if (a.in_lds == 4096) {
+        sort_kernel<1024, 4, 4><<<dim3(1 + fillers(a, 8, 1024)), dim3(1024), 0, stream>>>(a);
+    } else if (a.in_lds) {
+        sort_kernel<1024, 8, 4><<<dim3(1 + fillers(a, 8, 1024)), dim3(1024), 0, stream>>>(a);
     } else if (a.rounds == 1) {
         sort<1>(a, stream);
     } else if (a.rounds == 2) {
@@ -544,7 +552,7 @@ hipError_t launch_embedding_bwd(const void *id, const void *gy, const float *sca
     a.key1 = u32(p.key1); a.pos1 = u32(p.pos1); a.key2 = u32(p.key2); a.pos2 = u32(p.pos2);
     a.hist1 = u32(p.hist1); a.hist2 = u32(p.hist2);
     a.sums = reinterpret_cast<float *>(ws + p.sums);
-    a.n = p.n; a.V = p.V; a.C = p.C; a.bits = p.bits; a.bits1 = p.bits1; a.bits2 = p.bits2; a.rounds = p.rounds; a.blocks = p.blocks;
+    a.n = p.n; a.V = p.V; a.C = p.C; a.bits = p.bits; a.bits1 = p.bits1; a.bits2 = p.bits2; a.in_lds = p.in_lds; a.rounds = p.rounds; a.blocks = p.blocks;
     a.chunk = p.chunk; a.chunks = p.chunks; a.pieces = (uint32_t)C / 8;
     return bf16 ? embedding_bwd<rows::bf16>(a, stream) : embedding_bwd<float>(a, stream);
 }
