@@ -32,6 +32,7 @@ constexpr uint32_t kCounts = 16;                         // workgroups' counts o
 constexpr int kPlaces = 8;                               // rows in flight of the sums (4, 8, 16: the same in bf16; fp32, 16384 x 768: 73, 73, 87 us)
 // Tokens that one workgroup sorts in LDS, places for 1024, 4096 or 8192; an item is an id above its place, in 32 bits.  The whole gradient, us, so / through the four
 // launches of the sort over all: 30522 x 768, 1024 tokens 28 / 38, 1100 25 / 33, 4096 26 / 34, 8192 32 / 39; 30522 x 64, 2048 21 / 23, 6000 26 / 25.
+// Beyond 8192 it gains nothing: 9000 tokens 36 / 37, 16384 52 / 41.
 constexpr uint32_t places_in_lds(uint32_t n, uint32_t bits) { return n <= 1024 ? 1024 : n <= 4096 && bits <= 20 ? 4096 : n <= 8192 && bits <= 19 ? 8192 : 0; }
 // Sort over all: a workgroup takes 256 tokens up to the first, 512 up to the second, beyond 2048, as every workgroup reads the counts of all.  The whole gradient, us, by
 // 256 / 512 / 2048: of 768 channels, 16384 tokens (and the lookup) 57 / 58 / -; of 64 channels, 16384 tokens 27 / 27 / 39, 32768 36 / 34 / 43,
@@ -112,8 +113,9 @@ Plan plan_for(long long n, int V, int C) {
     p.bits2 = p.bits - p.bits1;
     p.rounds = p.n <= kOneRound ? 1 : p.n <= kTwoRounds ? 2 : 8;
     p.blocks = (p.n + p.rounds * 256 - 1) / (p.rounds * 256);
-    // 16 / 32 / 64 places: 1024 tokens of 768 channels 28 / 32 / 41 us, 4096 38 / 42 / 51, 16384 58 / 60 / 65; 32768 75.5 / 74.5 / 77.6, of 2048 channels 271 / 266 / 269
-    p.chunk = p.n <= 16384 ? 16 : 32;
+    // 8 / 16 / 32 / 64 places: 768 channels, 77 tokens 21 / 23 / - / -, 1024 22.5 / 24.4 / 28 / 37, 4096 25 / 26.5 / 30 / 39, 8192 31 / 31.5 / - / -, 16384 45 / 42.5 / 45 /
+    // 49 us; 32768 tokens - / 75.5 / 74.5 / 77.6, of 2048 channels - / 271 / 266 / 269
+    p.chunk = p.n <= 8192 ? 8 : p.n <= 16384 ? 16 : 32;
     p.chunks = (p.n + p.chunk - 1) / p.chunk;
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
