@@ -5,8 +5,8 @@
 // mean and var come from x again: the row is read anyway, and nothing but x has to be kept (DELTA's Assumptions 1-3: the backward pass reads stored
 // forward activations).  x may be a checkpoint in 8 bits (packed.hpp), read as it lies.
 //
-// Bound by memory, 3 reads or writes of the tensor for the gradients (6 bytes a value in bf16, 5.03 with x in 8 bits) and 2 forward.  Up to 2048 channels a wavefront owns a row and
-// keeps it in registers (backward: of few rows up to 1024); beyond, a workgroup does, eight channels a thread.  Workers are persistent over rows, the next
+// Bound by memory, 3 reads or writes of the tensor for the gradients (6 bytes a value in bf16, 5.03 with x in 8 bits) and 2 forward.  Up to 1024 channels, and backward
+// up to 2048 if there are many rows, a wavefront owns a row and keeps it in registers; beyond, a workgroup does, eight channels a thread.  Workers are persistent over rows, the next
 // row's loads in flight while one is worked on, and keep their sums of dgamma and dbeta in registers: a workgroup writes one partial sum of 2 C values and
 // a second kernel adds those in a fixed order (no atomics: a fixed function of the inputs).  All statistics and sums are fp32: the mean first,
 // then the variance of the centred values.
@@ -25,7 +25,8 @@ namespace ln {
 using packed::u32x2;
 using rows::f32x4;
 
-constexpr int kRowChannels = 2048, kMostChannels = 8192; // forward: a wavefront owns a row up to the first
+// Forward: a wavefront owns a row up to the first.  fp32, a wavefront's and a workgroup's, us: 768 channels, 16384 rows 21 and 25; 2048 channels, 8192 rows 33 and 31.
+constexpr int kRowChannels = 1024, kMostChannels = 8192;
 // Backward: whether a wavefront owns a row.  Up to 1024 channels always; up to 2048 if there are rows enough for 128 workgroups of them.  Both kernels, us, a
 // wavefront's first: 768 channels, 16384 rows 22 and 46; 1536 channels, 8192 rows 21 and 30; 2048 channels, 8192 rows 25 and 34; 1536 channels, 2048
 // rows 24 and 24, 77 rows 8.1 and 6.4; 2048 channels, 200 rows 13.4 and 12.8.
@@ -349,12 +350,8 @@ hipError_t launch_layernorm_more(const void *x, void *y, const float *gamma, con
     const long long groups = (rows + 3) / 4;
     const dim3 grid((unsigned)(groups < 4096 ? groups : 4096)), block(256);
     auto run = [&](auto kernel) { kernel<<<grid, block, 0, stream>>>(a); };
-    switch ((C + 511) / 512) {
-    case 1: run(ln::forward_kernel<float, 1>); break;
-    case 2: run(ln::forward_kernel<float, 2>); break;
-    case 3: run(ln::forward_kernel<float, 3>); break;
-    default: run(ln::forward_kernel<float, 4>); break;
-    }
+    if (C <= 512) run(ln::forward_kernel<float, 1>);
+    else run(ln::forward_kernel<float, 2>);
     return hipGetLastError();
 }
 

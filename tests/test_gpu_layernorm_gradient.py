@@ -76,7 +76,8 @@ def test_gradients_match_float64(torch_mod, rows, C, dtype):
 
 
 @pytest.mark.parametrize("rows,C,dtype", [(37, 768, "f32"), (1, 8, "f32"), (5, 2048, "f32"), (13, 1000, "f32"), (2, 8192, "f32"), (1030, 2112, "bf16"),
-                                          (3, 8192, "bf16"), (1, 4096, "bf16"), (17000, 64, "f32")])
+                                          (3, 8192, "bf16"), (1, 4096, "bf16"), (17000, 64, "f32"), (9, 1032, "f32"),
+                                          (1100, 1544, "f32"), (1, 2040, "f32")])
 def test_forward_in_fp32_and_over_wide_rows(torch_mod, rows, C, dtype):
     print("rows", rows, "C", C, dtype, flush=True)
     x, _, _, gamma, beta = _case(rows, C, dtype)
