@@ -27,7 +27,7 @@ namespace emb {
 
 using rows::f32x4;
 
-constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup, chunks of the joins
+constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup (1, 2, 4: the same within 1 us), chunks of the joins
 constexpr uint32_t kCounts = 16;                         // workgroups' counts of a digit in flight (8, 16, 32: 16384 tokens 45, 43, 42 us; 40000 119, 116, 117)
 constexpr int kPlaces = 8;                               // rows in flight of the sums (4, 8, 16: the same in bf16; fp32, 16384 x 768: 73, 73, 87 us)
 // Tokens that one workgroup sorts in LDS, places for 1024, 4096 or 8192; an item is an id above its place, in 32 bits.  The whole gradient, us, so / through the four
