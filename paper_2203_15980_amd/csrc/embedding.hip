@@ -34,10 +34,11 @@ constexpr int kPlaces = 8;                               // rows in flight of th
 // launches of the sort over all: 30522 x 768, 1024 tokens 28 / 38, 1100 25 / 33, 4096 26 / 34, 8192 32 / 39; 30522 x 64, 2048 21 / 23, 6000 26 / 25.
 // Beyond 8192 it gains nothing: 9000 tokens 36 / 37, 16384 52 / 41.
 constexpr uint32_t places_in_lds(uint32_t n, uint32_t bits) { return n <= 1024 ? 1024 : n <= 4096 && bits <= 20 ? 4096 : n <= 8192 && bits <= 19 ? 8192 : 0; }
-// Sort over all: a workgroup takes 256 tokens up to the first, 512 up to the second, beyond 2048, as every workgroup reads the counts of all.  The whole gradient, us, by
+// Sort over all: a workgroup takes 256 tokens up to the first, 512 up to the second, 2048 up to the third, beyond 8192, as every workgroup reads the counts of all.  The whole gradient, us, by
 // 256 / 512 / 2048: of 768 channels, 16384 tokens (and the lookup) 57 / 58 / -; of 64 channels, 16384 tokens 27 / 27 / 39, 32768 36 / 34 / 43,
-// 65536 46 / 39 / 46, 131072 69 / 53 / 49, 2097152 - / 1688 / 321.
-constexpr uint32_t kOneRound = 16384, kTwoRounds = 65536;
+// 65536 46 / 39 / 46, 131072 69 / 53 / 49, 2097152 - / 1688 / 321; of 16 channels, by 2048 / 8192, 1048576 136 / 153,
+// 2097152 305 / 230, 8388608 2139 / 871.
+constexpr uint32_t kOneRound = 16384, kTwoRounds = 65536, kEightRounds = 1 << 20;
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
 constexpr long long kMostTokens = 1 << 24;
 
@@ -111,7 +112,7 @@ Plan plan_for(long long n, int V, int C) {
     while ((1u << p.bits) <= (uint32_t)V) ++p.bits;
     p.bits1 = (p.bits + 1) / 2;
     p.bits2 = p.bits - p.bits1;
-    p.rounds = p.n <= kOneRound ? 1 : p.n <= kTwoRounds ? 2 : 8;
+    p.rounds = p.n <= kOneRound ? 1 : p.n <= kTwoRounds ? 2 : p.n <= kEightRounds ? 8 : 32;
     p.blocks = (p.n + p.rounds * 256 - 1) / (p.rounds * 256);
     // 8 / 16 / 32 / 64 places: 768 channels, 77 tokens 21 / 23 / - / -, 1024 22.5 / 24.4 / 28 / 37, 4096 25 / 26.5 / 30 / 39, 8192 31 / 31.5 / - / -, 16384 45 / 42.5 / 45 /
     // 49 us; 32768 tokens - / 75.5 / 74.5 / 77.6, of 2048 channels - / 271 / 266 / 269
@@ -529,8 +530,10 @@ static hipError_t embedding_bwd(const emb::Args &a, hipStream_t stream) {
         sort<1>(a, stream);
     } else if (a.rounds == 2) {
         sort<2>(a, stream);
-    } else {
+    } else if (a.rounds == 8) {
         sort<8>(a, stream);
+    } else {
+        sort<32>(a, stream);
     }
     const uint32_t threads = (a.pieces + 63) / 64 * 64;
     sums_kernel<T><<<dim3(a.chunks), dim3(threads), 0, stream>>>(a);

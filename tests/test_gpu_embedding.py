@@ -42,7 +42,8 @@ GRADIENT = [(1, 1, 8, "any"), (1, 100, 768, "any"), (63, 7, 64, "any"), (64, 2, 
             (16384, 2 ** 20, 8, "bad"), (16385, 3, 64, "same"), (16401, 7, 64, "runs"), (33, 7, 64, "same"), (48, 3, 64, "runs"), (65537, 3, 8, "same"),
             (16383, 300, 16, "falling"), (65536, 100, 8, "falling"), (65537, 2 ** 17, 16, "bad"), (200001, 3000, 8, "falling"),
             (4096, 2 ** 20 - 1, 8, "any"), (4096, 2 ** 20, 8, "bad"), (8192, 2 ** 19 - 1, 8, "bad"), (8191, 2 ** 19, 8, "any"), (8192, 2 ** 19, 8, "falling"),
-            (8193, 300, 64, "falling"), (8192, 3, 64, "runs"), (8192, 100, 64, "same"), (6001, 1, 8, "any"), (4095, 30, 64, "none")]
+            (8193, 300, 64, "falling"), (8192, 3, 64, "runs"), (8192, 100, 64, "same"), (6001, 1, 8, "any"), (4095, 30, 64, "none"),
+            (2 ** 20, 5000, 8, "falling"), (2 ** 20 + 1, 2 ** 22 - 1, 8, "bad"), (2 ** 20 + 8191, 5000, 8, "falling")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
