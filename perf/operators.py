@@ -246,7 +246,6 @@ def _prepare_own(case, v):
             p.put(n, v[n])
     i = p.ids
     p.forward, p.backward, p.out, p.v = None, [], [], v
-    p.several = k in ("layernorm", "embedding")                  # outputs that come as a list
     pack = dl.LayerDesc(x=i.get("x", 0), y=i.get("packed", 0), Cin=C, Cout=C, op=dl.OP_PACK8, pack=fmt, **geo)
     if k == "pack":
         p.forward = dl.layer_array([pack, dl.LayerDesc(x=i["packed"], y=i["y"], Cin=C, Cout=C, op=dl.OP_UNPACK8, pack=fmt, **geo)])
@@ -313,7 +312,7 @@ def run(state):
     if p.backward:
         p.d.backward_segment(p.backward)
         p.d.backward_join()
-    return p.out if p.several else p.out[0]
+    return p.out[0] if len(p.out) == 1 else p.out
 
 
 # ------------------------------------------------------------------ work
