@@ -285,6 +285,8 @@ def _prepare_own(case, v):
         if k == "layernorm":
             p.out.append(p.view("gx"))
         p.out.append(p.gw)
+    if k == "embedding" and len(p.out) == 1:
+        p.out = [p.out]                                          # a list also where it is one output, as in the plain form
     return p
 
 
