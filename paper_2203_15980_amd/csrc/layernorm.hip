@@ -215,8 +215,9 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
     }
     const float over = 1.0f / (float)a.C;
     auto work = [&](uint32_t row, int d) {
-        // with c = x - mean and u = gy * rstd * gamma: gx = u - mean(u) - c * rstd^2 * mean(u * c), and gy * xh = gy * rstd * c
-        float c[R][8], u[R][8];
+        // gx = g * rstd - mean(g) * rstd - xh * (mean(g * xh) * rstd): rstd never meets itself, so that a row's gradient is finite wherever rstd is (its square
+        // leaves fp32 for var + eps below 2^-128), and two multiply-adds a value make it
+        float c[R][8], g[R][8];                          // x - mean, then xh
         rows::Eight<T> gc[R], ar[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -235,18 +236,18 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
             if constexpr (LDS) load8(gamma + (ck0 + STRIDE * r) * 8, gm);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float t = scaled(gy[e], rstd);
-                dg[r][e] += t * c[r][e];
+                c[r][e] = scaled(c[r][e], rstd);
+                dg[r][e] += gy[e] * c[r][e];
                 db[r][e] += gy[e];
-                u[r][e] = scaled(t, LDS ? gm[e] : kept[e]);
-                s1 += u[r][e];
-                s2 += u[r][e] * c[r][e];
+                g[r][e] = scaled(gy[e], LDS ? gm[e] : kept[e]);
+                s1 += g[r][e];
+                s2 += g[r][e] * c[r][e];
             }
         }
         sum.two(s1, s2, slots + 32);
         if (!a.gx) return;
-        s1 = scaled(s1, over);
-        s2 = scaled(scaled(s2, over), scaled(rstd, rstd));
+        s1 = scaled(scaled(s1, over), rstd);
+        s2 = scaled(scaled(s2, over), rstd);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (!live[r]) continue;
@@ -254,7 +255,7 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
             if constexpr (ADD) ar[r].to(add);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                o[e] = (u[r][e] - s1) - c[r][e] * s2;
+                o[e] = __builtin_fmaf(-c[r][e], s2, __builtin_fmaf(g[r][e], rstd, -s1));
                 if constexpr (ADD) o[e] += add[e];
             }
             rows::Eight<T>::store(a.gx + (uint64_t)row * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)), o);
