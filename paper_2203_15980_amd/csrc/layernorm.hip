@@ -29,7 +29,12 @@ using rows::f32x4;
 constexpr int kRowChannels = 1024, kMostChannels = 8192;
 // Backward: whether a wavefront owns a row.  Up to 1024 channels always; up to 2048 if there are rows enough for 128 workgroups of them.  Both kernels, us, a
 // wavefront's first: 768 channels, 16384 rows 22 and 46; 1536 channels, 8192 rows 21 and 30; 2048 channels, 8192 rows 25 and 34; 1536 channels, 2048
-// rows 24 and 24, 77 rows 8.1 and 6.4; 2048 channels, 200 rows 13.4 and 12.8.
+// rows 24 and 24, 77 rows 8.1 and 6.4; 2048 channels, 200 rows 13.4 and 12.8.  The same by type and input, from int8 (E4M3 within 1 us of it) behind the semicolon,
+// with gx_add in brackets:
+//   2048 channels, 8192 rows: bf16 25 and 34 (31 and 41); 23 and 34 (27 and 38), fp32 50 and 47 (59 and 57); 40 and 40 (52 and 49)
+//   1544 channels, 8192 rows: bf16 22 and 33 (26 and 36); 21 and 34 (24 and 36), fp32 38 and 39 (49 and 48); 28 and 35 (42 and 43)
+//   2048 channels, 1024 rows: bf16 11.6 and 13.7 (12.5 and 14.2); 12.2 and 14.2 (12.3 and 14.1), fp32 13.6 and 15.1 (14.7 and 16.2); 13.2 and 14.7 (14.9 and 15.4)
+// fp32 with gx_add keeps its row in registers because gx_add is fetched late: fetched with the row 24 to 63 registers went to memory, and 85 us to the 59.
 constexpr bool row_to_wave(long long rows, int C) { return C <= 1024 || (C <= 2048 && rows >= 1024); }
 // Wavefronts of its workgroup.  The same for a tensor and its checkpoint, with and without gx_add: the sums' order, and so their bits, do not depend on those.
 // us with 8 and 16: 512 channels, 16384 rows 16.2 and 15.8; 768 channels, bf16 21.4 and 20.3, fp32 52 and 56 (forward too), 77 rows 7.0 and 8.2.
@@ -188,6 +193,7 @@ __global__ __launch_bounds__(1024) void forward_wide_kernel(Args a) {
 template <typename T, int FMT, bool ADD, bool LDS, int R, int STRIDE, int DEEP, typename SUM>
 __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint32_t step, uint32_t ck0, const SUM &sum, float *slots, const float *gamma,
                                               float (&dg)[R][8], float (&db)[R][8]) {
+    constexpr bool kLate = R >= 4 && sizeof(T) == 4;     // gx_add is fetched where it is added, or the row does not fit the registers
     bool live[R];
     float kept[8];
 #pragma unroll
@@ -223,7 +229,7 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
         for (int r = 0; r < R; ++r) {
             xr[d][r].to(c[r]);
             gc[r] = gr[d][r];
-            if (ADD && live[r]) ar[r].load(a.add + (uint64_t)row * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)));
+            if (ADD && !kLate && live[r]) ar[r].load(a.add + (uint64_t)row * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)));
         }
         if (row + DEEP * step < a.rows) fetch(row + DEEP * step, d);
         const float rstd = centre<R>(c, live, a, over, sum, slots);
@@ -252,6 +258,7 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
         for (int r = 0; r < R; ++r) {
             if (!live[r]) continue;
             float o[8], add[8];
+            if constexpr (ADD && kLate) ar[r].load(a.add + (uint64_t)row * a.C * sizeof(T) + (ck0 + STRIDE * r) * (8u * (uint32_t)sizeof(T)));
             if constexpr (ADD) ar[r].to(add);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
