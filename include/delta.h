@@ -175,6 +175,7 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * chip, probabilities rounded to bf16 before they multiply v).  W = S = stride = 1, pad = 0.
  * DELTA_OP_LAYERNORM: y = (x - mean) / sqrt(var + eps) * scale + shift over the Cin (= Cout) channels of each of
  * the N*H*W rows, a multiple of 8 up to 2048 or a multiple of 64 up to 8192; scale = gamma, shift = beta (16-byte aligned).
+ * Rows: 2147483647 at most, four times as many forward in bf16 up to 2048 channels.
  * Attention is bf16 only, layer normalisation bf16 or fp32; both ignore w and take no res.
  * DELTA_OP_EMBEDDING: y[m,k] = scale_k * w[id[m]][k] over m in N*H*W tokens (at most 16777216): x holds their ids, int64, Cin = the rows of
  * the table (at most 4194303), Cout = its channels (a multiple of 8 up to 8192), w = the table [Cin][Cout] in the storage type, bf16 or fp32,

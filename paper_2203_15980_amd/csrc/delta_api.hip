@@ -1377,6 +1377,7 @@ delta_status prepare_backward_stem(delta_ctx *c, const delta_bwd_desc &D, uint32
 }
 
 // Layer normalisation and the embedding: bf16 and fp32, gradients of the input, of the weights or of both, and a workspace for the latter.
+bool too_many_rows(const delta_layer_desc &L) { return (uint64_t)L.N * L.H * L.W > 0x7FFFFFFFull; }      // the gradients' kernels number them in 32 bits
 uint64_t row_op_workspace_bytes(const delta_layer_desc &L) {
     const long long rows = (long long)L.N * L.H * L.W;
     const uint64_t need = L.op == DELTA_OP_LAYERNORM ? delta::layernorm_bwd_workspace_bytes(rows, L.Cin) : delta::embedding_bwd_workspace_bytes(rows, L.Cin, L.Cout);
@@ -1391,6 +1392,7 @@ delta_status prepare_backward_rows(delta_ctx *c, const delta_bwd_desc &D, uint32
     if (r != DELTA_OK) return r;
     const size_t nt = c->tensors.size();
     const bool norm = L.op == DELTA_OP_LAYERNORM;
+    if (too_many_rows(L)) return fail(c, DELTA_ERR_INVALID, "backward %u: gradients are made over at most 2147483647 rows", i);
     if (D.mask_gx || D.gy_masked) return fail(c, DELTA_ERR_INVALID, "backward %u: this operator has no masks", i);
     if (D.gy >= nt || c->tensors[D.gy].bytes != c->tensors[L.y].bytes || D.gpre != D.gy)
         return fail(c, DELTA_ERR_INVALID, "backward %u: gy must have the bytes of y and gpre must be gy", i);
@@ -1706,7 +1708,11 @@ delta_status delta_backward_workspace(delta_ctx *c, const delta_layer_desc *laye
     delta::PoolArgs pa;
     uint64_t flops = 0;
     if ((r = prepare_layer(c, *layer, 0, a, pa, flops, true)) != DELTA_OK) return r;
-    if (layer->op == DELTA_OP_LAYERNORM || layer->op == DELTA_OP_EMBEDDING) { *out_bytes = row_op_workspace_bytes(*layer); return DELTA_OK; }
+    if (layer->op == DELTA_OP_LAYERNORM || layer->op == DELTA_OP_EMBEDDING) {
+        if (too_many_rows(*layer)) return fail(c, DELTA_ERR_INVALID, "layer 0: gradients are made over at most 2147483647 rows");
+        *out_bytes = row_op_workspace_bytes(*layer);
+        return DELTA_OK;
+    }
     if (layer->op != DELTA_OP_CONV) { *out_bytes = 0; return DELTA_OK; }
     if (is_stem(*layer)) { *out_bytes = delta::stem_wgrad_workspace_bytes(a); return DELTA_OK; }
     as_stride_1(*layer, a);

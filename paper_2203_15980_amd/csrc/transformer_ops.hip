@@ -20,6 +20,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 static constexpr int kRounds = 4;               // 8 channels x 64 lanes x 4 rounds = 2048 channels
 static constexpr int kRowsPerBlock = 4;
+static constexpr long long kRowsPerLaunch = 1LL << 25;      // a launch holds fewer than 2^32 threads: of 64 to a row, 2^26 rows
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -86,12 +87,12 @@ __global__ __launch_bounds__(kRowsPerBlock * 64) void layernorm_kernel(const uns
 
 const char *layernorm_check(const void *x, const void *y, const float *gamma, const float *beta, long long rows, int C,
                             int bf16) {
-    (void)bf16;
+    const bool narrow = bf16 && C <= tops::kRounds * 512;    // this file's kernel; layernorm.hip's number their rows in 32 bits
     if (rows <= 0 || C <= 0 || C % 8 || C > 8192 || (C > tops::kRounds * 512 && C % 64))
         return "channels must be a multiple of 8 up to 2048, a multiple of 64 up to 8192";
     if (!x || !y || !gamma || !beta || (((uintptr_t)x | (uintptr_t)y | (uintptr_t)gamma | (uintptr_t)beta) & 15))
         return "pointers must be non-null and 16-byte aligned";
-    if (rows > 0x7FFFFFFFLL) return "too many rows";
+    if (rows > 0x7FFFFFFFLL * (narrow ? tops::kRowsPerBlock : 1)) return "too many rows";
     return nullptr;
 }
 
@@ -99,10 +100,16 @@ hipError_t launch_layernorm(const void *x, void *y, const float *gamma, const fl
                             float eps, int bf16, hipStream_t stream) {
     if (layernorm_check(x, y, gamma, beta, rows, C, bf16)) return hipErrorInvalidValue;
     if (!bf16 || C > tops::kRounds * 512) return launch_layernorm_more(x, y, gamma, beta, rows, C, eps, bf16, stream);
-    const unsigned blocks = (unsigned)((rows + tops::kRowsPerBlock - 1) / tops::kRowsPerBlock);
-    tops::layernorm_kernel<<<dim3(blocks), dim3(tops::kRowsPerBlock * 64), 0, stream>>>(
-        static_cast<const unsigned char *>(x), static_cast<unsigned char *>(y), gamma, beta, rows, C, eps);
-    return hipGetLastError();
+    for (long long at = 0; at < rows; at += tops::kRowsPerLaunch) {
+        const long long n = rows - at < tops::kRowsPerLaunch ? rows - at : tops::kRowsPerLaunch;
+        const unsigned blocks = (unsigned)((n + tops::kRowsPerBlock - 1) / tops::kRowsPerBlock);
+        const size_t from = (size_t)at * C * 2;
+        tops::layernorm_kernel<<<dim3(blocks), dim3(tops::kRowsPerBlock * 64), 0, stream>>>(
+            static_cast<const unsigned char *>(x) + from, static_cast<unsigned char *>(y) + from, gamma, beta, n, C, eps);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace delta
