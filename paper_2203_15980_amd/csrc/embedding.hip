@@ -75,13 +75,16 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
     const uint32_t step = gridDim.x * a.side;
     for (uint32_t m0 = blockIdx.x * a.side + at; m0 < a.n; m0 += kLookups * step) {
         rows::Eight<T> raw[kLookups];
+        bool there[kLookups];
 #pragma unroll
         for (int i = 0; i < kLookups; ++i) {
             const uint32_t m = m0 + i * step;
             raw[i].zero();
+            there[i] = false;
             if (m >= a.n) continue;
             const int64_t id = a.id[m];
-            if ((uint64_t)id < a.V) raw[i].load(a.w + ((uint64_t)id * a.C + piece * 8) * sizeof(T));
+            there[i] = (uint64_t)id < a.V;
+            if (there[i]) raw[i].load(a.w + ((uint64_t)id * a.C + piece * 8) * sizeof(T));
         }
 #pragma unroll
         for (int i = 0; i < kLookups; ++i) {
@@ -90,7 +93,7 @@ __global__ __launch_bounds__(1024) void lookup_kernel(LookupArgs a) {
             float v[8];
             raw[i].to(v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= f[e];
+            for (int e = 0; e < 8; ++e) v[e] = there[i] ? v[e] * f[e] : 0.f;       // zero also where the factor is an infinity or a NaN
             rows::Eight<T>::store(a.y + ((uint64_t)m * a.C + piece * 8) * sizeof(T), v);
         }
     }
