@@ -12,8 +12,10 @@
 //     workgroups' digit counts itself.  (One workgroup for 16384 tokens, or sixteen with an id's low bits each, took 23 us where the four launches took 20.)
 //   * sums: a workgroup owns a chunk of sorted places, whose rows of gy it fetches 8 at a time, and adds up run by run.  A run of one id
 //     that begins and ends in the chunk is a row of gw; what a chunk holds of a run that goes on beyond it becomes a partial sum: its first run in slot 0
-//     if it came in from the chunk before, its last in slot 1 if it began here.  However often an id occurs, a chain is a chunk long.
-//   * joins: the chunk in which a run of several chunks begins adds its slot 1 and the following chunks' slots 0 up to the run's end, a row of gw.
+//     if it came in from the chunk before, its last in slot 1 if it began here.
+//   * joins: the chunk in which a run of several chunks begins adds its slot 1 and the following chunks' slots 0 up to the run's end, a row of gw.  Where
+//     that may be many, spans of about the square root of their number that lie inside one run are added up before, each by a workgroup of its own: an id that all
+//     tokens hold costs a chain of at most 256 chunks, or of four spans, and its sum is rounded that often.
 // us for V = 30522, C = 768, bf16, 16384 tokens: lookup 13 (50 MB, 4 TB/s), sort with zeros 28 (94 MB written, 3.4 TB/s), sums 12, joins 4.5; V = 131072,
 // C = 2048, 32768 tokens: 180 (1.07 GB, 6.0 TB/s), 62, 6.
 #include <hip/hip_runtime.h>
@@ -39,6 +41,13 @@ constexpr uint32_t places_in_lds(uint32_t n, uint32_t bits) { return n <= 1024 ?
 // 65536 46 / 39 / 46, 131072 69 / 53 / 49, 2097152 - / 1688 / 321; of 16 channels, by 2048 / 8192, 1048576 136 / 153,
 // 2097152 305 / 230, 8388608 2139 / 871.
 constexpr uint32_t kOneRound = 16384, kTwoRounds = 65536, kEightRounds = 1 << 20;
+// Joins: groups of threads that share a run's chunks, and how many chunks to a group are joined at once, by one workgroup; of more, spans of chunks that one run
+// covers are joined ahead, in a launch of their own.  At once a run over all tokens takes 64 loads one after the other (half a microsecond each) to 256 chunks a
+// group.  The whole gradient, us, at once / by spans: ids all different 16384 x 768 (205 chunks a group) 46 / 47.2, 8192 x 2048 (1024) 61 / 62.4, 32768 x 2048
+// 113 / 116, 131072 x 64 (512) 50 / 52; half of the tokens one id 57 / 47, 124 / 72, 179 / 122, 87 / 53; all of them 72 / 45, 190 / 64, 241 / 114, 120 / 47.
+// 16777216 x 16, all one id: 16035 / 1625.
+inline uint32_t groups_of(uint32_t pieces) { return pieces >= 256 ? 1 : 512 / pieces < 8 ? 512 / pieces : 8; }
+constexpr uint32_t kJoinedAtOnce = 256;
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
 constexpr long long kMostTokens = 1 << 24;
 
@@ -105,6 +114,7 @@ struct Plan {
     uint32_t n, V, C;
     uint32_t bits, bits1, bits2;                         // of a key and its two digits; an id of no token sorts as V, behind all others
     uint32_t rounds, blocks, chunk, chunks;
+    uint32_t span;                                       // chunks that are joined ahead where one run covers them all, or 0: none are
     uint64_t key1, pos1, key2, pos2, hist1, hist2, sums, bytes;                    // workspace: byte offsets and size
 };
 
@@ -121,6 +131,9 @@ Plan plan_for(long long n, int V, int C) {
     // 49 us; 32768 tokens - / 75.5 / 74.5 / 77.6, of 2048 channels - / 271 / 266 / 269
     p.chunk = p.n <= 8192 ? 8 : p.n <= 16384 ? 16 : 32;
     p.chunks = (p.n + p.chunk - 1) / p.chunk;
+    p.span = 0;
+    if (p.chunks > kJoinedAtOnce * groups_of(p.C / 8))   // about the square root: as many spans to a table's longest run as chunks to a span
+        for (p.span = 2; (uint64_t)p.span * p.span < p.chunks; p.span *= 2) {}
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
     p.in_lds = places_in_lds(p.n, p.bits);
@@ -139,7 +152,7 @@ struct Args {
     float *gw;
     uint32_t *key1, *pos1, *key2, *pos2, *hist1, *hist2;
     float *sums;                                         // [chunks][2][C]
-    uint32_t n, V, C, bits, bits1, bits2, in_lds, rounds, blocks, chunk, chunks, pieces;
+    uint32_t n, V, C, bits, bits1, bits2, in_lds, rounds, blocks, chunk, chunks, span, pieces;
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t id, uint32_t V) { return (uint64_t)id < V ? (uint32_t)id : V; }
@@ -427,28 +440,14 @@ __global__ __launch_bounds__(1024) void sums_kernel(Args a) {
     close(run == after);
 }
 
-// The runs that begin in this workgroup's chunk and go on into the next: slot 1 of this chunk, then slots 0 of the following ones that begin with the same id.
-// Threads: `side` groups of `pieces`; group g adds every side-th of those chunks, and the groups' sums are added in their order.
-__global__ __launch_bounds__(1024) void joins_kernel(Args a, uint32_t side) {
-    extern __shared__ __align__(16) float part[];        // [side][C]
-    const uint32_t next = (blockIdx.x + 1) * a.chunk, key = a.key2[next];          // one workgroup fewer than there are chunks
-    if (key >= a.V || a.key2[next - 1] != key) return;
-    if (blockIdx.x && a.key2[next - a.chunk] == key && a.key2[next - a.chunk - 1] == key) return;      // it began further back
-    uint32_t following = 0;                              // chunks that begin with this id, 64 looked at together
-    for (;;) {
-        const uint64_t at = (uint64_t)(blockIdx.x + 1 + following + (threadIdx.x & 63)) * a.chunk;
-        const uint64_t others = __ballot(at >= a.n || a.key2[at] != key);
-        if (others) {
-            following += (uint32_t)__builtin_ctzll(others);
-            break;
-        }
-        following += 64;
-    }
+// Adds up rows place(0), place(1), .. of the partial sums.  Threads: `side` groups of `pieces`; group g adds every side-th row, kAhead of them in flight, and
+// group 0 the groups' sums in their order (`part`: [side][C]).  Only group 0 returns true, and holds the sum.
+template <typename PLACE>
+__device__ __forceinline__ bool add_up(const Args &a, uint32_t side, uint32_t places, PLACE place, float *part, float (&sum)[8]) {
     const uint32_t piece = threadIdx.x % a.pieces, group = threadIdx.x / a.pieces;
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
     if (group < side) {
-        // place 0 is this chunk's slot 1, place j the j-th following chunk's slot 0
-        const uint32_t places = following + 1;
         for (uint32_t j0 = group; j0 < places; j0 += side * kAhead) {
             f32x4 v[kAhead][2];
 #pragma unroll
@@ -456,7 +455,7 @@ __global__ __launch_bounds__(1024) void joins_kernel(Args a, uint32_t side) {
                 const uint32_t j = j0 + k * side;
                 v[k][0] = v[k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if (j >= places) continue;
-                const f32x4 *at = reinterpret_cast<const f32x4 *>(a.sums + ((uint64_t)(blockIdx.x + j) * 2 + (j ? 0 : 1)) * a.C + piece * 8);
+                const f32x4 *at = reinterpret_cast<const f32x4 *>(a.sums + (uint64_t)place(j) * a.C + piece * 8);
                 v[k][0] = at[0];
                 v[k][1] = at[1];
             }
@@ -468,11 +467,64 @@ __global__ __launch_bounds__(1024) void joins_kernel(Args a, uint32_t side) {
         put(part + (uint64_t)group * a.C + piece * 8, sum);
     }
     __syncthreads();
-    if (group) return;
+    if (group) return false;
     for (uint32_t g = 1; g < side; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += part[g * a.C + piece * 8 + e];
-    float f[8];
+    return true;
+}
+
+// A span of chunks that lies inside one run: the sum of its slots 0 into slot 1 of its first chunk, which is free, as the run came in.
+__global__ __launch_bounds__(1024) void spans_kernel(Args a, uint32_t side) {
+    extern __shared__ __align__(16) float part[];
+    const uint32_t first = blockIdx.x * a.span, key = a.key2[first * a.chunk];     // whole spans only: all their chunks are there
+    if (!first || key >= a.V || a.key2[first * a.chunk - 1] != key || a.key2[(first + a.span - 1) * a.chunk] != key) return;
+    float sum[8];
+    if (add_up(a, side, a.span, [&](uint32_t j) { return (first + j) * 2; }, part, sum))
+        put(a.sums + ((uint64_t)first * 2 + 1) * a.C + threadIdx.x % a.pieces * 8, sum);
+}
+
+// The runs that begin in this workgroup's chunk and go on into the next: slot 1 of this chunk, then slots 0 of the following ones that begin with the same id,
+// or for a whole span of them slot 1 of its first.
+template <bool SPANS>
+__global__ __launch_bounds__(1024) void joins_kernel(Args a, uint32_t side) {
+    extern __shared__ __align__(16) float part[];
+    const uint32_t next = (blockIdx.x + 1) * a.chunk, key = a.key2[next];          // one workgroup fewer than there are chunks
+    if (key >= a.V || a.key2[next - 1] != key) return;
+    if (blockIdx.x && a.key2[next - a.chunk] == key && a.key2[next - a.chunk - 1] == key) return;      // it began further back
+    // Chunks that begin with this id: 64 are looked at together, and if all do, first every 4096th, then every 64th, then each.
+    const uint32_t from = blockIdx.x + 1;
+    uint32_t following = 0;
+    auto look = [&](uint32_t apart) {                    // how many of the next 64 groups of `apart` chunks begin with it to their last
+        const uint64_t at = (uint64_t)(from + following + ((threadIdx.x & 63) + 1) * apart - 1) * a.chunk;
+        const uint64_t others = __ballot(at >= a.n || a.key2[at] != key);
+        const uint32_t groups = others ? (uint32_t)__builtin_ctzll(others) : 64;
+        following += groups * apart;
+        return groups;
+    };
+    if (look(1) == 64)
+        for (uint32_t apart = 4096; apart; apart /= 64)
+            while (look(apart) == 64) {}
+    // place 0 is this chunk's slot 1; then `before` chunks, `spans` spans, the rest chunks
+    uint32_t before = following, spans = 0, first = 0;
+    if constexpr (SPANS) {
+        const uint32_t lo = (from + a.span - 1) / a.span, hi = (from + following) / a.span;
+        if (lo < hi) {
+            before = lo * a.span - from;
+            spans = hi - lo;
+            first = lo * a.span;
+        }
+    }
+    const uint32_t behind = before + spans, places = SPANS ? 1 + behind + (following - before - spans * a.span) : 1 + following;
+    auto place = [&](uint32_t j) {
+        if (!j) return blockIdx.x * 2 + 1;
+        if (!SPANS || j <= before) return (blockIdx.x + j) * 2;
+        if (j <= behind) return (first + (j - before - 1) * a.span) * 2 + 1;
+        return (first + spans * a.span + (j - behind - 1)) * 2;
+    };
+    float sum[8], f[8];
+    if (!add_up(a, side, places, place, part, sum)) return;
+    const uint32_t piece = threadIdx.x;                  // of group 0
     factors(a.scale, piece, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] *= f[e];
@@ -541,8 +593,15 @@ static hipError_t embedding_bwd(const emb::Args &a, hipStream_t stream) {
     const uint32_t threads = (a.pieces + 63) / 64 * 64;
     sums_kernel<T><<<dim3(a.chunks), dim3(threads), 0, stream>>>(a);
     if (a.chunks > 1) {
-        const uint32_t side = a.pieces >= 256 ? 1 : 512 / a.pieces < 8 ? 512 / a.pieces : 8;
-        joins_kernel<<<dim3(a.chunks - 1), dim3((a.pieces * side + 63) / 64 * 64), side * a.C * sizeof(float), stream>>>(a, side);
+        const uint32_t side = groups_of(a.pieces);
+        const dim3 block((a.pieces * side + 63) / 64 * 64);
+        const size_t lds = side * a.C * sizeof(float);
+        if (a.span) {
+            spans_kernel<<<dim3(a.chunks / a.span), block, lds, stream>>>(a, side);
+            joins_kernel<true><<<dim3(a.chunks - 1), block, lds, stream>>>(a, side);
+        } else {
+            joins_kernel<false><<<dim3(a.chunks - 1), block, lds, stream>>>(a, side);
+        }
     }
     return hipGetLastError();
 }
@@ -561,7 +620,7 @@ hipError_t launch_embedding_bwd(const void *id, const void *gy, const float *sca
     a.hist1 = u32(p.hist1); a.hist2 = u32(p.hist2);
     a.sums = reinterpret_cast<float *>(ws + p.sums);
     a.n = p.n; a.V = p.V; a.C = p.C; a.bits = p.bits; a.bits1 = p.bits1; a.bits2 = p.bits2; a.in_lds = p.in_lds; a.rounds = p.rounds; a.blocks = p.blocks;
-    a.chunk = p.chunk; a.chunks = p.chunks; a.pieces = (uint32_t)C / 8;
+    a.chunk = p.chunk; a.chunks = p.chunks; a.span = p.span; a.pieces = (uint32_t)C / 8;
     return bf16 ? embedding_bwd<rows::bf16>(a, stream) : embedding_bwd<float>(a, stream);
 }
 

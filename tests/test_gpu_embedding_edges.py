@@ -1,8 +1,8 @@
-"""The embedding at its edges: factors that are infinities or NaN."""
+"""The embedding at its edges: factors that are infinities or NaN, ids that very many tokens hold."""
 import numpy as np
 import pytest
 
-from rowops_util import Bench, storage, values
+from rowops_util import EPS24, Bench, storage, values
 
 pytestmark = pytest.mark.gpu
 
@@ -42,4 +42,54 @@ def test_no_token_is_zero_whatever_the_factors_are(torch_mod, C, dtype):
     occurs = np.isin(np.arange(V), ids[there])
     assert not occurs[V - 2:].any()
     assert np.array_equal(gw.cpu().numpy().reshape(V, C), np.where(occurs[:, None], sums * scale, 0.0), equal_nan=True)
+    b.close()
+
+
+EVERYWHERE = [(16384, 768, "all"), (8192, 2048, "half"), (30000, 2056, "runs"), (1 << 17, 2048, "all"), (1 << 22, 8, "all"), (1 << 22, 16, "half"), ((1 << 20) + 77, 264, "runs"), (40000, 1032, "runs"), (1 << 16, 8192, "half")]
+
+
+@pytest.mark.parametrize("n,C,kind", EVERYWHERE)
+def test_the_row_of_a_frequent_id_is_as_exact_as_others(torch_mod, n, C, kind):
+    """An id that very many tokens hold: fp32 values of one sign, against float64.  A chunk's chain is 8, 16 or 32 additions; `side` groups (8 up to 512 channels,
+    one from 2048 on) join up to 256 chunks each at once.  Of more, s being the power of two next above the square root of the chunks, spans of s are joined ahead
+    in chains of s / side + side, then at most 3 s of chunks, spans, chunks; one more rounding for the factor, each half a step of the sum of magnitudes."""
+    torch = torch_mod
+    print("tokens", n, "C", C, kind, flush=True)
+    V = 11
+    g = torch.Generator("cuda:0").manual_seed(n + C)
+    ids = torch.full((n,), 5, device="cuda:0", dtype=torch.int64)
+    if kind == "half":
+        some = torch.rand(n, device="cuda:0", generator=g) < 0.5
+        ids[some] = torch.randint(0, V, (int(some.sum()),), device="cuda:0", generator=g)
+    if kind == "runs":                                       # long runs whose ends lie anywhere, some short, an id of no token among them
+        ids = torch.tensor([1, 4, 4, 4, 9, 9, -1, 0], device="cuda:0")[torch.randint(0, 8, (n,), device="cuda:0", generator=g)]
+        ids[:40] = 10
+    b = Bench(torch, [n * 8, n * C * 4, n * C * 4])
+    view = lambda i, t: b.arena[b.at[i]:b.at[i] + b.sizes[i]].view(t)          # noqa: E731
+    view(0, torch.int64).copy_(ids)
+    gy = view(2, torch.float32).view(n, C)
+    value = 0.05 + torch.rand(C, device="cuda:0", generator=g)                 # one value to a channel: every addition of a chain rounds the same way
+    gy.copy_(value[None])
+    scale = np.full(C, 1.5, np.float32)
+    s = b.dev(scale)
+    fwd = b.layer(b.dl.OP_EMBEDDING, n, V, C, 0, 1, "f32", w=s.data_ptr(), scale=s.data_ptr())
+    ws, _ = b.workspace(b.d.backward_workspace(fwd))
+    runs = []
+    for fill in (0x7F, 0x00):
+        ws.fill_(fill)
+        gw, guard = b.guarded(V * C)
+        torch.cuda.synchronize()
+        b.d.backward_segment([b.bwd(fwd, 2, gw=gw, ws=ws)])
+        b.d.sync()
+        runs.append(gw.clone())
+    assert torch.equal(runs[0], runs[1])
+    count = torch.bincount(ids[ids >= 0], minlength=V).double()
+    want = count[:, None] * value.double()[None] * 1.5
+    chunk, side = 8 if n <= 8192 else 16 if n <= 16384 else 32, 1 if C >= 2048 else min(8, 512 // (C // 8))
+    chunks, span = -(-n // chunk), 2
+    while span * span < chunks:
+        span *= 2
+    chain = chunk + (chunks / side if chunks <= 256 * side else 4 * span / side + side) + side + 1
+    off = (runs[0].view(V, C).double() - want).abs() / want.clamp(min=1e-30)
+    assert float(off.max()) <= chain * EPS24, (float(off.max()) / EPS24, chain)
     b.close()
