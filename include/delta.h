@@ -184,7 +184,7 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * half (a quarter of fp32).  DELTA_OP_PACK8 writes y, the checkpoint of x over N*H*W rows of Cin channels; DELTA_OP_UNPACK8 restores a tensor from a
  * checkpoint x; `pack` names the format, delta_packed_bytes the checkpoint's size.  A checkpoint is a tensor of the table like any other: it is released,
  * offloaded and reloaded, and its parent in a graph is the tensor it was made from.  A row's channels go in blocks of 32 (the last of a row may be
- * shorter); a block has one scale 2^e, e the smallest integer from -120 on for which no value of it exceeds 127 * 2^e (DELTA_PACK_INT8) or 448 * 2^e
+ * shorter; at most 536870911 blocks); a block has one scale 2^e, e the smallest integer from -120 on for which no value of it exceeds 127 * 2^e (DELTA_PACK_INT8) or 448 * 2^e
  * (DELTA_PACK_E4M3); a value is x / 2^e rounded, ties to even, to a whole number or to an OCP E4M3 number.  A block with an infinity or a NaN
  * reads back as NaN throughout; what rounds up to 2^128 as an infinity.  What comes back is exact in bf16 and fp32, so a backward operator that reads the checkpoint works on the same
  * values as one that reads the unpacked tensor.  Layout: N*H*W * Cin bytes (q in two's complement, or the E4M3 code), padded to 16; then e + 127 for each block,

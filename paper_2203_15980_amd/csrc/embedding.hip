@@ -16,8 +16,8 @@
 //   * joins: the chunk in which a run of several chunks begins adds its slot 1 and the following chunks' slots 0 up to the run's end, a row of gw.  Where
 //     that may be many, spans of about the square root of their number that lie inside one run are added up before, each by a workgroup of its own: an id that all
 //     tokens hold costs a chain of at most 256 chunks, or of four spans, and its sum is rounded that often.
-// us for V = 30522, C = 768, bf16, 16384 tokens: lookup 13 (50 MB, 4 TB/s), sort with zeros 28 (94 MB written, 3.4 TB/s), sums 12, joins 4.5; V = 131072,
-// C = 2048, 32768 tokens: 180 (1.07 GB, 6.0 TB/s), 62, 6.
+// us for V = 30522, C = 768, bf16, 16384 tokens: lookup 13 (50 MB, 4 TB/s; 8 with the table's rows in the caches), sort with zeros 28.5 (94 MB written,
+// 3.3 TB/s), sums 12, joins 4.3; V = 131072, C = 2048, 32768 tokens: 181 (1.07 GB, 5.9 TB/s), 63, spans 4.7, joins 6.  fp32, 16384 tokens: lookup 14.5.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -30,22 +30,30 @@ namespace emb {
 using rows::f32x4;
 
 constexpr int kLookups = 2, kAhead = 4;                  // rows in flight of the lookup (1, 2, 4: the same within 1 us), chunks of the joins
-constexpr uint32_t kCounts = 16;                         // workgroups' counts of a digit in flight (8, 16, 32: 16384 tokens 45, 43, 42 us; 40000 119, 116, 117)
+constexpr uint32_t kCounts = 16;                         // workgroups' counts in flight (8, 16, 32: 16384 tokens 45, 43, 42 us; 40000 119, 116, 117)
 constexpr int kPlaces = 8;                               // rows in flight of the sums (4, 8, 16: the same in bf16; fp32, 16384 x 768: 73, 73, 87 us)
-// Tokens that one workgroup sorts in LDS, places for 1024, 4096 or 8192; an item is an id above its place, in 32 bits.  The whole gradient, us, so / through the four
-// launches of the sort over all: 30522 x 768, 1024 tokens 28 / 38, 1100 25 / 33, 4096 26 / 34, 8192 32 / 39; 30522 x 64, 2048 21 / 23, 6000 26 / 25.
-// Beyond 8192 it gains nothing: 9000 tokens 36 / 37, 16384 52 / 41.
-constexpr uint32_t places_in_lds(uint32_t n, uint32_t bits) { return n <= 1024 ? 1024 : n <= 4096 && bits <= 20 ? 4096 : n <= 8192 && bits <= 19 ? 8192 : 0; }
-// Sort over all: a workgroup takes 256 tokens up to the first, 512 up to the second, 2048 up to the third, beyond 8192, as every workgroup reads the counts of all.  The whole gradient, us, by
-// 256 / 512 / 2048: of 768 channels, 16384 tokens (and the lookup) 57 / 58 / -; of 64 channels, 16384 tokens 27 / 27 / 39, 32768 36 / 34 / 43,
-// 65536 46 / 39 / 46, 131072 69 / 53 / 49, 2097152 - / 1688 / 321; of 16 channels, by 2048 / 8192, 1048576 136 / 153,
-// 2097152 305 / 230, 8388608 2139 / 871.
+// Tokens that one workgroup sorts in LDS, places for 1024, 4096 or 8192; an item is an id above its place, in 32 bits.  The whole gradient, us, so and
+// through the four launches of the sort over all workgroups:
+//   tokens        1024      1100      4096      8192      9000      16384    | of 64 channels: 2048      6000
+//   30522 x 768   28 / 38   25 / 33   26 / 34   32 / 39   36 / 37   52 / 41  | 21 / 23   26 / 25
+constexpr uint32_t places_in_lds(uint32_t n, uint32_t bits) {
+    return n <= 1024 ? 1024 : n <= 4096 && bits <= 20 ? 4096 : n <= 8192 && bits <= 19 ? 8192 : 0;
+}
+// Sort over all workgroups: each takes 256 tokens up to the first number, 512 up to the second, 2048 up to the third, 8192 beyond, as each reads the
+// counts of all.  The whole gradient, us:
+//   tokens, channels   16384, 768 (and the lookup)   16384, 64   32768, 64   65536, 64   131072, 64   1048576, 16   2097152, 64   2097152, 16   8388608, 16
+//   256                57                            27          36          46          69
+//   512                58                            27          34          39          53                         1688
+//   2048                                             39          43          46          49           136           321           305           2139
+//   8192                                                                                              153                         230           871
 constexpr uint32_t kOneRound = 16384, kTwoRounds = 65536, kEightRounds = 1 << 20;
-// Joins: groups of threads that share a run's chunks, and how many chunks to a group are joined at once, by one workgroup; of more, spans of chunks that one run
-// covers are joined ahead, in a launch of their own.  At once a run over all tokens takes 64 loads one after the other (half a microsecond each) to 256 chunks a
-// group.  The whole gradient, us, at once / by spans: ids all different 16384 x 768 (205 chunks a group) 46 / 47.2, 8192 x 2048 (1024) 61 / 62.4, 32768 x 2048
-// 113 / 116, 131072 x 64 (512) 50 / 52; half of the tokens one id 57 / 47, 124 / 72, 179 / 122, 87 / 53; all of them 72 / 45, 190 / 64, 241 / 114, 120 / 47.
-// 16777216 x 16, all one id: 16035 / 1625.
+// Joins: groups of threads that share a run's chunks, and how many chunks to a group are joined at once, by one workgroup; of more, spans of chunks that
+// one run covers are joined ahead, in a launch of their own.  At once a run over all tokens takes 64 loads one after the other (half a microsecond each)
+// to 256 chunks a group.  The whole gradient, us, at once and by spans:
+//   tokens x channels (chunks a group)   16384 x 768 (205)   8192 x 2048 (1024)   32768 x 2048 (1024)   131072 x 64 (512)   16777216 x 16 (65536)
+//   ids all different                    46 / 47             60 / 62              113 / 116             50 / 52             1710 / 1711
+//   half of the tokens one id            57 / 47             124 / 72             179 / 122             92 / 53             8740 / 1688
+//   all of them                          72 / 45             190 / 65             241 / 115             131 / 48            16080 / 1624
 inline uint32_t groups_of(uint32_t pieces) { return pieces >= 256 ? 1 : 512 / pieces < 8 ? 512 / pieces : 8; }
 constexpr uint32_t kJoinedAtOnce = 256;
 constexpr int kMostBits = 22, kMostBins = 1 << ((kMostBits + 1) / 2);
@@ -127,8 +135,11 @@ Plan plan_for(long long n, int V, int C) {
     p.bits2 = p.bits - p.bits1;
     p.rounds = p.n <= kOneRound ? 1 : p.n <= kTwoRounds ? 2 : p.n <= kEightRounds ? 8 : 32;
     p.blocks = (p.n + p.rounds * 256 - 1) / (p.rounds * 256);
-    // 8 / 16 / 32 / 64 places: 768 channels, 77 tokens 21 / 23 / - / -, 1024 22.5 / 24.4 / 28 / 37, 4096 25 / 26.5 / 30 / 39, 8192 31 / 31.5 / - / -, 16384 45 / 42.5 / 45 /
-    // 49 us; 32768 tokens - / 75.5 / 74.5 / 77.6, of 2048 channels - / 271 / 266 / 269
+    // us, 768 channels:  77 tokens   1024   4096   8192   16384   32768   | of 2048 channels: 32768
+    //   8 places         21          22.5   25     31     45
+    //   16               23          24.4   26.5   31.5   42.5    75.5    | 271
+    //   32                           28     30            45      74.5    | 266
+    //   64                           37     39            49      77.6    | 269
     p.chunk = p.n <= 8192 ? 8 : p.n <= 16384 ? 16 : 32;
     p.chunks = (p.n + p.chunk - 1) / p.chunk;
     p.span = 0;

@@ -5,13 +5,14 @@
 // mean and var come from x again: the row is read anyway, and nothing but x has to be kept (DELTA's Assumptions 1-3: the backward pass reads stored
 // forward activations).  x may be a checkpoint in 8 bits (packed.hpp), read as it lies.
 //
-// Bound by memory, 3 reads or writes of the tensor for the gradients (6 bytes a value in bf16, 5.03 with x in 8 bits) and 2 forward.  Up to 1024 channels, and backward
-// up to 2048 if there are many rows, a wavefront owns a row and keeps it in registers; beyond, a workgroup does, eight channels a thread.  Workers are persistent over rows, the next
-// row's loads in flight while one is worked on, and keep their sums of dgamma and dbeta in registers: a workgroup writes one partial sum of 2 C values and
-// a second kernel adds those in a fixed order (no atomics: a fixed function of the inputs).  All statistics and sums are fp32: the mean first,
-// then the variance of the centred values.
-// us, and the second kernel's beside them, with 16384 rows of 768 channels: bf16 17 + 4 (75 MB, 4.4 TB/s; from int8 17 + 4), fp32 27 + 5 (151 MB, 5.6 TB/s), forward
-// 21 (100 MB, 4.8 TB/s); 8192 rows of 8192 channels with gx_add, bf16 108 + 7 (537 MB, 5.0 TB/s), forward 61 (268 MB, 4.4 TB/s); 77 rows of 768 4.6 + 2.3.
+// Bound by memory, 3 reads or writes of the tensor for the gradients (6 bytes a value in bf16, 5.03 with x in 8 bits) and 2 forward.  Up to 1024
+// channels, and backward up to 2048 if there are many rows, a wavefront owns a row and keeps it in registers; beyond, a workgroup does, eight channels a
+// thread.  Workers are persistent over rows, the next row's loads in flight while one is worked on, and keep their sums of dgamma and dbeta in
+// registers: a workgroup writes one partial sum of 2 C values and a second kernel adds those in a fixed order (no atomics: a fixed function of the
+// inputs).  All statistics and sums are fp32: the mean first, then the variance of the centred values.
+// us, and the second kernel's beside them, with 16384 rows of 768 channels: bf16 17.5 + 4 (75 MB, 4.3 TB/s; from int8 or E4M3, 63 MB, the same), fp32 27 + 4.5
+// (151 MB, 5.6 TB/s), forward 21.5 (100 MB, 4.7 TB/s); 8192 rows of 8192 channels with gx_add, bf16 110 + 7 (537 MB, 4.9 TB/s), forward 62 (268 MB, 4.3 TB/s);
+// 8192 rows of 2048 channels with gx_add, fp32, 49 + 5 (268 MB, 5.4 TB/s), forward 29 (134 MB, 4.7 TB/s); 77 rows of 768 4.7 + 2.3.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -25,22 +26,29 @@ namespace ln {
 using packed::u32x2;
 using rows::f32x4;
 
-// Forward: a wavefront owns a row up to the first.  fp32, a wavefront's and a workgroup's, us: 768 channels, 16384 rows 21 and 25; 2048 channels, 8192 rows 33 and 31.
+// Forward: a wavefront owns a row up to the first.  fp32, a wavefront's and a workgroup's, us: 768 channels, 16384 rows 21 and 25; 2048 channels, 8192
+// rows 33 and 31.
 constexpr int kRowChannels = 1024, kMostChannels = 8192;
-// Backward: whether a wavefront owns a row.  Up to 1024 channels always; up to 2048 if there are rows enough for 128 workgroups of them.  Both kernels, us, a
-// wavefront's first: 768 channels, 16384 rows 22 and 46; 1536 channels, 8192 rows 21 and 30; 2048 channels, 8192 rows 25 and 34; 1536 channels, 2048
-// rows 24 and 24, 77 rows 8.1 and 6.4; 2048 channels, 200 rows 13.4 and 12.8.  The same by type and input, from int8 (E4M3 within 1 us of it) behind the semicolon,
-// with gx_add in brackets:
-//   2048 channels, 8192 rows: bf16 25 and 34 (31 and 41); 23 and 34 (27 and 38), fp32 50 and 47 (59 and 57); 40 and 40 (52 and 49)
-//   1544 channels, 8192 rows: bf16 22 and 33 (26 and 36); 21 and 34 (24 and 36), fp32 38 and 39 (49 and 48); 28 and 35 (42 and 43)
-//   2048 channels, 1024 rows: bf16 11.6 and 13.7 (12.5 and 14.2); 12.2 and 14.2 (12.3 and 14.1), fp32 13.6 and 15.1 (14.7 and 16.2); 13.2 and 14.7 (14.9 and 15.4)
-// fp32 with gx_add keeps its row in registers because gx_add is fetched late: fetched with the row 24 to 63 registers went to memory, and 85 us to the 59.
+// Backward: whether a wavefront owns a row.  Up to 1024 channels always; up to 2048 if there are rows enough for 128 workgroups of them.  Both kernels, us,
+// a wavefront's first, from int8 (E4M3 within 1 us of it) and with gx_add:
+//   rows x channels   bf16          with gx_add   from int8     with gx_add   fp32          with gx_add   from int8     with gx_add
+//   16384 x 768       22 and 46
+//   8192 x 1544       22 and 33     26 and 36     21 and 34     24 and 36     38 and 39     49 and 48     28 and 35     42 and 43
+//   8192 x 2048       25 and 34     31 and 41     23 and 34     27 and 38     50 and 47     59 and 57     40 and 40     52 and 49
+//   2048 x 1536       24 and 24
+//   1024 x 2048       11.6, 13.7    12.5, 14.2    12.2, 14.2    12.3, 14.1    13.6, 15.1    14.7, 16.2    13.2, 14.7    14.9, 15.4
+//   200 x 2048        13.4, 12.8
+//   77 x 1536         8.1, 6.4
+// In fp32 with gx_add a row of 2048 stays in registers because gx_add is fetched late: fetched with the row 24 to 63 registers went to memory, and 85 us
+// to the 59.
 constexpr bool row_to_wave(long long rows, int C) { return C <= 1024 || (C <= 2048 && rows >= 1024); }
 // Wavefronts of its workgroup.  The same for a tensor and its checkpoint, with and without gx_add: the sums' order, and so their bits, do not depend on those.
-// us with 8 and 16: 512 channels, 16384 rows 16.2 and 15.8; 768 channels, bf16 21.4 and 20.3, fp32 52 and 56 (forward too), 77 rows 7.0 and 8.2.
+// us with 8 and 16: 512 channels, 16384 rows 16.2 and 15.8; 768 channels, bf16 21.4 and 20.3, fp32 52 and 56 (forward too), 77 rows 7.0 and 8.2: there 8, as
+// bf16 with many rows gains less than the others lose.
 template <int R> constexpr int kWaves = R == 1 ? 16 : 8;
 
-// Rows fetched ahead, by a wavefront (1 and 2: 768 channels 21.4 and 21.3 us, fp32 52 and 54) and by a workgroup (1 and 2: 8192 channels, with the forward pass, 188 and 178).
+// Rows fetched ahead, by a wavefront (1 and 2: 768 channels 21.4 and 21.3 us, fp32 52 and 54) and by a workgroup (1 and 2: 8192 channels, with the
+// forward pass, 188 and 178).
 constexpr int kDeep = 1, kDeepWide = 2;
 
 struct Args {

@@ -3,8 +3,8 @@
 //
 // Bound by memory: 3.03 bytes a value in bf16, 5.03 in fp32, one read and one write of each.  A thread owns eight channels (16 or 32 bytes on one side,
 // 8 on the other), the four threads of a block of 32 find its largest magnitude with two exchanges inside the quad, and each thread has
-// kAhead such pieces in flight.  us for 16384 x 768, pack and unpack: bf16 (38 MB each) with 1, 2, 4, 8 pieces 7.7 + 7.6, 6.6 + 6.8 (5.7 TB/s), 9.0 + 7.9, 10.3 + 9.7;
-// fp32 (63 MB) 14.9 + 13.2, 16.3 + 13.1, 17.0 + 13.1, 18.4 + 14.5.
+// kAhead such pieces in flight.  us for 16384 x 768, pack and unpack, with 1, 2, 4, 8 pieces: bf16 (38 MB each) 7.7 + 7.6, 6.6 + 6.8 (5.7 TB/s),
+// 9.0 + 7.9, 10.3 + 9.7; fp32 (63 MB) 14.9 + 13.2 (11 + 13 on tensors that the caches partly hold), 16.3 + 13.1, 17.0 + 13.1, 18.4 + 14.5.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

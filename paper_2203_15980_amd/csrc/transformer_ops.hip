@@ -88,6 +88,7 @@ __global__ __launch_bounds__(kRowsPerBlock * 64) void layernorm_kernel(const uns
 const char *layernorm_check(const void *x, const void *y, const float *gamma, const float *beta, long long rows, int C,
                             int bf16) {
     const bool narrow = bf16 && C <= tops::kRounds * 512;    // this file's kernel; layernorm.hip's number their rows in 32 bits
+    // layernorm.hip's kernels run any multiple of 8: beyond 2048 channels whole pieces of 64 are asked for, as calls with 2056 were refused before those were there
     if (rows <= 0 || C <= 0 || C % 8 || C > 8192 || (C > tops::kRounds * 512 && C % 64))
         return "channels must be a multiple of 8 up to 2048, a multiple of 64 up to 8192";
     if (!x || !y || !gamma || !beta || (((uintptr_t)x | (uintptr_t)y | (uintptr_t)gamma | (uintptr_t)beta) & 15))

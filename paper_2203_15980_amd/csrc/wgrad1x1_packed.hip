@@ -6,16 +6,18 @@
 //  * gpre, the bytes of x and its scale bytes go from memory straight into LDS through a ring of S slices of 128 pixels (64 beside four k tiles), 48 KB a
 //    slice of 128 x 128 where bf16 needs 64; one barrier a slice.
 //  * x stays in 8 bits as far as the registers: gfx950's transposing read of bytes (ds_read_b64_tr_b8: 16 lanes point at 8 rows of 16 channels, each
-//    gets one channel's 8 values along the rows) gives a lane the 8 pixels of one MFMA operand, which it converts: 20 instructions for 8 values in
-//    int8, 16 in E4M3.  So that these hide behind the MFMAs a wavefront owns 128 x 64 of (k, c) where K allows: 8 MFMAs (256 cycles) for
-//    40 conversions (160).  The pixels' scales are turned into bf16 once a slice, a slice ahead, and read by whole wavefronts at once (in
-//    fp32 these reads were half of all LDS reads).
+//    gets one channel's 8 values along the rows) gives a lane the 8 pixels of one MFMA operand, which it converts, two values and their two scales with
+//    7 instructions in int8, 6 in E4M3: 28 and 24 for 8 values.  A wavefront owns 128 x 64 of (k, c) where K allows, so that a step is 8 MFMAs (256
+//    cycles) beside the next step's 56 conversions (224).  The first step of a slice is converted before its first product, with nothing beside it: with two
+//    steps a slice (128 x 128) that is half of all conversions, with one (64 channels of x) all.  The pixels' scales are turned into bf16 once a slice,
+//    a slice ahead, and read by whole wavefronts at once (in fp32 these reads were half of all LDS reads).
 //    With x converted by the whole workgroup into a bf16 tile a slice ahead instead, and 64 x 64 to a wavefront, a slice's steps waited for one
 //    another: 43 us for 768 -> 768 on 16384 tokens.
 //  * Workgroups are numbered so that those of one split, which read the same pixels, are on one XCD and share its L2: a third of the misses.
 //  * The wavefronts that share a tile add their sums through LDS, in a fixed tree.
-// us, and the reduction's beside them: 768 -> 768 on 16384 tokens, int8, 35 + 5.5 (550 TFLOP/s; E4M3 33; wgrad1x1.hip on the unpacked tensor 40 + 5.5), on 333 tokens
-// 1024 -> 256 9 + 2.  Bound by neither memory (38 MB, 6 us) nor the matrix units (8) alone: a slice's waits, LDS reads and conversions beside the products.
+// us, and the reduction's beside them: 768 -> 768 on 16384 tokens, int8, 35 + 5.4 (550 TFLOP/s; E4M3 33; wgrad1x1.hip on the unpacked tensor 40 + 5.5), on 333
+// tokens 1024 -> 256 9 + 3.4.  Bound by neither memory (38 MB, 6 us) nor the matrix units (8) alone: a slice's waits, LDS reads, and the conversions that
+// stand before the products or between them.
 // Rows past the last pixel are fetched from the last pixel and overwritten with zeros in LDS; their scales are zeros.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(512) void wgrad1x1_packed_kernel(Args a) {
     }
 }
 
-// A workgroup's time per pixel, and what one more split of a 128 x 128 tile costs: wgrad1x1.hip's.
+// A workgroup's time per pixel, and what one more split of a 128 x 128 tile costs: wgrad1x1.hip's, taken over as they are, not measured for this kernel.
 static constexpr double kPixelNs = 5.5, kSumsNs = 24.;
 
 struct Plan { int kt, ct, tiles, nslices, nsplit; };
