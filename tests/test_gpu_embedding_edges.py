@@ -93,3 +93,50 @@ def test_the_row_of_a_frequent_id_is_as_exact_as_others(torch_mod, n, C, kind):
     off = (runs[0].view(V, C).double() - want).abs() / want.clamp(min=1e-30)
     assert float(off.max()) <= chain * EPS24, (float(off.max()) / EPS24, chain)
     b.close()
+
+
+def test_long_runs_captured_into_a_graph_and_replayed_with_other_ids(torch_mod):
+    """The gradient whose spans are joined ahead, captured; each replay finds other ids in place: runs elsewhere, none, one over all tokens.  Whole numbers:
+    equality with sums made on the device."""
+    torch, n, V, C = torch_mod, 40000, 50, 1032
+    stream = torch.cuda.Stream()
+    b = Bench(torch, [n * 8, n * C * 2, n * C * 2], stream=stream)
+    view = lambda i, t: b.arena[b.at[i]:b.at[i] + b.sizes[i]].view(t)          # noqa: E731
+    g = torch.Generator("cuda:0").manual_seed(3)
+    gy = view(2, torch.bfloat16).view(n, C)
+    gy.copy_(torch.randint(-8, 9, (n, C), device="cuda:0", generator=g))
+    s = b.dev(np.full(C, 2.0, np.float32))
+    fwd = b.layer(b.dl.OP_EMBEDDING, n, V, C, 0, 1, w=s.data_ptr(), scale=s.data_ptr())
+    ws, _ = b.workspace(b.d.backward_workspace(fwd))
+    gw, guard = b.guarded(V * C)
+    desc = b.bwd(fwd, 2, gw=gw, ws=ws)
+    ids = view(0, torch.int64)
+    ids.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        b.d.backward_segment([desc])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        b.d.backward_segment([desc])
+    for k in range(5):
+        now = torch.randint(0, V, (n,), device="cuda:0", generator=g)
+        if k in (1, 4):
+            now[torch.rand(n, device="cuda:0", generator=g) < 0.7] = 7 * k
+        if k == 2:
+            now[:] = V - 1
+        if k == 3:
+            now = torch.sort(torch.randint(-1, 4, (n,), device="cuda:0", generator=g)).values
+        ids.copy_(now)
+        gw.fill_(float("nan"))
+        ws.fill_(0x7F if k % 2 else 0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.zeros(V, C, device="cuda:0")
+        there = now >= 0
+        want.index_add_(0, now[there], gy[there].float() * 2)
+        assert torch.equal(gw.view(V, C), want), k
+        assert bool((guard[:64] == 12345.0).all()) and bool((guard[64 + V * C:] == 12345.0).all())
+    del graph
+    b.close()
