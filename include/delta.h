@@ -77,8 +77,15 @@ enum {
     DELTA_OP_ADD = 8,        /* y = x + res (bf16) */
     DELTA_OP_PACK8 = 9,      /* x into its checkpoint in 8 bits */
     DELTA_OP_UNPACK8 = 10,   /* a checkpoint back into a tensor */
-    DELTA_OP_EMBEDDING = 11  /* rows of a table by token ids, times a factor */
+    DELTA_OP_EMBEDDING = 11, /* rows of a table by token ids, times a factor */
+    DELTA_OP_RMSNORM = 12,   /* root-mean-square normalisation over the channel axis (+ residual in front, + checkpoint of the result) */
+    DELTA_OP_ROTARY = 13,    /* rotary positions with several axes */
+    DELTA_OP_ATTENTION_PACKED = 14, /* attention over packed sequences, causal or not, grouped heads (bf16, heads of 64 or 128) */
+    DELTA_OP_LOGPROB = 15    /* log probabilities of given tokens, entropy, log-sum-exp, most likely tokens */
 };
+/* Field `flags` of a layer. */
+enum { DELTA_ATTENTION_CAUSAL = 1 /* DELTA_OP_ATTENTION_PACKED: a position sees itself and those before it */,
+       DELTA_ROTARY_PAIRS = 1 /* DELTA_OP_ROTARY: channels (2 i, 2 i + 1) are a pair, not (i, i + D / 2) */ };
 /* Checkpoint formats (field `pack` of a layer). */
 enum { DELTA_PACK_NONE = 0, DELTA_PACK_INT8 = 1, DELTA_PACK_E4M3 = 2 };
 enum { DELTA_SYNC_D2H = 1, DELTA_SYNC_H2D = 2, DELTA_SYNC_COMPUTE = 4, DELTA_SYNC_ALL = 7 };
@@ -180,6 +187,26 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * DELTA_OP_EMBEDDING: y[m,k] = scale_k * w[id[m]][k] over m in N*H*W tokens (at most 16777216): x holds their ids, int64, Cin = the rows of
  * the table (at most 4194303), Cout = its channels (a multiple of 8 up to 8192), w = the table [Cin][Cout] in the storage type, bf16 or fp32,
  * scale = a factor per channel (a constant one for the usual sqrt(Cout)).  An id outside [0, Cin) stands for no token: its row of y is zero.
+ * A decoder layer's operators (N * H * W rows; y2 and y3 are further outputs, DELTA_NO_TENSOR where there is none):
+ * DELTA_OP_RMSNORM (bf16 and fp32, Cin = Cout a multiple of 8 up to 8192): s = x + res, rounded to the storage type and stored in y2; without res s = x and y2
+ * is DELTA_NO_TENSOR.  y = s / sqrt(mean(s^2) + eps) * scale over the channels of each row; scale = gamma (fp32, 16-byte aligned), no shift.  The sum of
+ * squares is fp32: finite for |s| up to 2^63 / sqrt(Cin).  With `pack`, y3 receives y's checkpoint, the bits that DELTA_OP_PACK8 makes of y;
+ * without, y3 is DELTA_NO_TENSOR.
+ * DELTA_OP_ROTARY (bf16 and fp32): x, y [rows][(R + S) D], R rotated heads, then S copied ones, of D channels, a multiple of 16 up to 256.  res: positions,
+ * int64 [rows][A], A from 1 to 8 by the tensor's bytes; scale: fp32 frequencies [A][D / 2] in radians a position.  theta_i = sum_a pos_a * scale[a][i]; pair i of a
+ * rotated head's channels, (i, i + D / 2) or with DELTA_ROTARY_PAIRS (2 i, 2 i + 1), becomes (u cos theta_i - v sin theta_i, u sin theta_i + v cos theta_i).
+ * Frequencies that are zero but for one axis give each pair of channels its axis.  Angles are formed in 64 bits and reduced there: exact to fp32 up to
+ * 2^31 radians.
+ * DELTA_OP_ATTENTION_PACKED (bf16): x [rows][(R + 2 S) D] = R heads of queries, S of keys, S of values, R a multiple of S, D = 64 or 128; res: offsets, int64,
+ * one more than there are sequences (by the tensor's bytes): sequence i is the rows from offset i up to offset i + 1, ascending, possibly none.
+ * y [rows][Cout = R D] = softmax(q k^T / sqrt(D)) v over the sequence's rows, with DELTA_ATTENTION_CAUSAL over those up to the query's own; head h reads key head
+ * h / (R / S).  y2: log-sum-exp of the scaled scores, fp32 [R][rows] (the gradient needs it), or DELTA_NO_TENSOR.  Rows of no sequence are not read, and zero
+ * in y and y2.  Offsets are known to the device alone: ones that do not ascend or leave [0, rows] give results that mean nothing, but no access outside the tensors.
+ * An infinity or a NaN in a row may reach any row of its sequence, and no other sequence.  Its flops are not counted in delta_stats.
+ * DELTA_OP_LOGPROB (bf16 and fp32): logits x [rows][Cin], any Cin; res: token ids, int64 [rows]; y fp32 [3][rows]: the ids' log probabilities, the entropy, the
+ * log-sum-exp.  Cout = K, 0 to 64: y2 (fp32 [rows][K]) the largest log probabilities, descending, y3 (int64 [rows][K]) their ids, of equal logits the lowest id
+ * first, a NaN above all; K = 0: both DELTA_NO_TENSOR.  An id outside [0, Cin) stands for no token: that row of y and y2 is zero, of y3 -1.  A logit of
+ * -infinity has no weight; a row of nothing else has log probabilities and log-sum-exp -infinity and entropy 0; a NaN or +infinity makes its row NaN.
  * Checkpoints in 8 bits (bf16 or fp32, Cin = Cout a multiple of 8): beside Evict and Offload a third way to make an activation small, to about a
  * half (a quarter of fp32).  DELTA_OP_PACK8 writes y, the checkpoint of x over N*H*W rows of Cin channels; DELTA_OP_UNPACK8 restores a tensor from a
  * checkpoint x; `pack` names the format, delta_packed_bytes the checkpoint's size.  A checkpoint is a tensor of the table like any other: it is released,
@@ -208,7 +235,10 @@ typedef struct {
     float eps;                 /* DELTA_OP_LAYERNORM and DELTA_OP_BATCHNORM */
     uint32_t fuse;             /* DELTA_FUSE_* bits (convolutions only; 0 everywhere else) */
     uint32_t pack;             /* DELTA_PACK_*: the format of y (DELTA_OP_PACK8) or of x (DELTA_OP_UNPACK8; in a backward descriptor
-                                  also DELTA_OP_LAYERNORM and linear layers); 0 everywhere else */
+                                  also DELTA_OP_LAYERNORM and linear layers) or of y3 (DELTA_OP_RMSNORM); 0 everywhere else */
+    uint32_t y2, y3;           /* further outputs of DELTA_OP_RMSNORM, DELTA_OP_ATTENTION_PACKED and DELTA_OP_LOGPROB, DELTA_NO_TENSOR for none (DELTA_OP_ROTARY:
+                                  both); other operators do not look at them */
+    uint32_t flags;            /* DELTA_ATTENTION_CAUSAL, DELTA_ROTARY_PAIRS; 0 everywhere else */
 } delta_layer_desc;
 
 typedef struct {
@@ -361,6 +391,15 @@ delta_status delta_set_skip_copies(delta_ctx *ctx, int32_t skip);
  *                      are required, gx and gx_add must be unset; needs fwd.x (the ids) resident; gpre = gy.  Sums in a fixed order.
  *   a linear layer     (DELTA_OP_CONV, 1x1, stride 1, bf16) with fwd.pack: as above, fwd.x being a checkpoint that the weight gradient reads;
  *                      no mask_gx.
+ *   DELTA_OP_RMSNORM   (bf16 and fp32) gx = r (g - sh mean(g sh)) (+ gx_add) per row, g = gy scale, r = 1 / sqrt(mean(s^2) + eps), sh = s r: the gradient of x and of
+ *                      res alike; gx_add, the gradient that s has from elsewhere, is added before the one rounding.  gw (fp32, Cin values)
+ *                      dgamma = sum gy sh; needs a workspace.  gx or gw may be left out.  Needs s resident: fwd.y2, or fwd.x without fwd.res.
+ *   DELTA_OP_ROTARY    (bf16 and fp32) gx = gy turned back, by -theta.  Needs fwd.res (positions) resident, not fwd.x.  No gw, no gx_add.
+ *   DELTA_OP_ATTENTION_PACKED (bf16) gx, all of it: of queries, keys and values, the latter two summed over the heads that read them in a fixed order; zero in rows of
+ *                      no sequence.  Needs fwd.x, fwd.res (offsets), fwd.y and fwd.y2 (log-sum-exp) resident, and a workspace.  No gw, no gx_add.
+ *   DELTA_OP_LOGPROB   (bf16 and fp32) gy fp32 [3][rows], the gradients of the log probability, the entropy and the log-sum-exp: gx_j = gy_0 ([j = id] - p_j)
+ *                      - gy_1 p_j (log p_j + entropy) + gy_2 p_j; zero in rows without a token or without weight.  Needs fwd.x, fwd.res (ids) and fwd.y
+ *                      resident.  No gradient of the alternatives, no gw, no gx_add.
  *   DELTA_OP_RELU      (bf16) gx = gy * [y > 0] on the stored output; needs fwd.y resident; gpre = gy.
  *   the stem           (DELTA_OP_CONV, 7x7, stride 2, pad 3, 3 -> 64 channels, bf16): weight gradient only
  *                      (gw required, fp32 [64][7][7][3]; gx, gx_add must be unset); gpre (bytes of y) receives
@@ -390,8 +429,8 @@ typedef struct delta_bwd_desc {
     const void *wt;            /* device: weights prepared by delta_bwd_weights (needed when gx is set) */
     void *gw;                  /* device, fp32 [Cout][R][S][Cin] (other operators: above): receives dL/dw (overwritten), or NULL */
     void *workspace;           /* device scratch, 256-byte aligned: the weight gradient's partial sums (from
-                                  its start; at its end where both gradients are made in one pass, and for layer
-                                  normalisation and the embedding) and,
+                                  its start; at its end where both gradients are made in one pass, and for both
+                                  normalisations, the embedding and attention) and,
                                   for a strided 1x1 layer, its staging tensor (at its end); needed when gw is
                                   set or (strided 1x1) gx is set.  A layer whose bytes at the end (staging, or
                                   the sums of one pass) overlap what weight gradients still in flight use makes

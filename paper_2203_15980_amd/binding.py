@@ -19,6 +19,8 @@ WGRAD_S2_MAX_Q = 51     # output columns up to which a 3x3 stride-2 layer's weig
 OP_CONV, OP_MAXPOOL, OP_AVGPOOL, OP_SOFTMAX_CE, OP_ATTENTION, OP_LAYERNORM = 0, 1, 2, 3, 4, 5
 OP_BATCHNORM, OP_RELU, OP_ADD = 6, 7, 8
 OP_PACK8, OP_UNPACK8, OP_EMBEDDING = 9, 10, 11
+OP_RMSNORM, OP_ROTARY, OP_ATTENTION_PACKED, OP_LOGPROB = 12, 13, 14, 15
+ATTENTION_CAUSAL, ROTARY_PAIRS = 1, 1
 PACK_NONE, PACK_INT8, PACK_E4M3 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 FUSE_NONE, FUSE_BLOCK, FUSE_NO_STORE = 0, 1, 2
@@ -60,7 +62,7 @@ class LayerDesc(C.Structure):
                 ("N", C.c_int32), ("H", C.c_int32), ("W", C.c_int32), ("Cin", C.c_int32),
                 ("Cout", C.c_int32), ("R", C.c_int32), ("S", C.c_int32), ("stride", C.c_int32),
                 ("pad", C.c_int32), ("relu", C.c_uint32), ("op", C.c_uint32), ("eps", C.c_float),
-                ("fuse", C.c_uint32), ("pack", C.c_uint32)]
+                ("fuse", C.c_uint32), ("pack", C.c_uint32), ("y2", C.c_uint32), ("y3", C.c_uint32), ("flags", C.c_uint32)]
 
 
 class BwdDesc(C.Structure):

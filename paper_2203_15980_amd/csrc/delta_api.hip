@@ -767,6 +767,11 @@ static uint64_t input_bytes(const delta_layer_desc &L) {
     return (uint64_t)L.N * L.H * L.W * L.Cin * (L.dtype == DELTA_DTYPE_BF16 ? 2 : 4);
 }
 
+// The operators that look at y2 and y3.
+static bool decoder_op(const delta_layer_desc &L) {
+    return L.op == DELTA_OP_RMSNORM || L.op == DELTA_OP_ROTARY || L.op == DELTA_OP_ATTENTION_PACKED || L.op == DELTA_OP_LOGPROB;
+}
+
 // Shape and size checks of one layer; fills the launch arguments except device addresses.  `backward`: the layer of a backward descriptor, whose x may
 // be a checkpoint where its operator reads one.
 static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint32_t i, delta::ConvArgs &a,
@@ -783,12 +788,23 @@ static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint3
     const uint64_t es = bf16 ? 2 : 4;
     const bool packs = L.op == DELTA_OP_PACK8 || L.op == DELTA_OP_UNPACK8;
     if (L.pack > DELTA_PACK_E4M3 || (packs && !L.pack)) return fail(c, DELTA_ERR_INVALID, "layer %u: unknown checkpoint format %u", i, L.pack);
-    if (L.pack && !packs && !(backward && (L.op == DELTA_OP_LAYERNORM || L.op == DELTA_OP_CONV)))
+    if (L.pack && !packs && L.op != DELTA_OP_RMSNORM && !(backward && (L.op == DELTA_OP_LAYERNORM || L.op == DELTA_OP_CONV)))
         return fail(c, DELTA_ERR_INVALID, "layer %u: a checkpoint is read by DELTA_OP_UNPACK8 and by the backward of layer normalisation and of linear "
                     "layers only", i);
+    if (L.flags && !((L.op == DELTA_OP_ATTENTION_PACKED || L.op == DELTA_OP_ROTARY) && L.flags == 1))
+        return fail(c, DELTA_ERR_INVALID, "layer %u: unknown flags %u", i, L.flags);
+    if (decoder_op(L)) {                             // the further outputs: tensors of their own
+        const uint32_t ids[5] = {L.x, L.res, L.y, L.y2, L.y3};
+        for (int j = 3; j < 5; ++j) {
+            if (ids[j] == DELTA_NO_TENSOR) continue;
+            if (ids[j] >= nt) return fail(c, DELTA_ERR_INVALID, "layer %u: tensor id out of range", i);
+            for (int k = 0; k < j; ++k)
+                if (ids[j] == ids[k]) return fail(c, DELTA_ERR_INVALID, "layer %u: a further output aliases an input or an output", i);
+        }
+    }
     const long long rows = (long long)L.N * L.H * L.W;
     const uint64_t plain = input_bytes(L), held = L.pack ? delta::packed_bytes((uint64_t)rows, (uint64_t)L.Cin) : 0;
-    const uint64_t xbytes = L.op == DELTA_OP_EMBEDDING ? (uint64_t)rows * 8 : L.pack && L.op != DELTA_OP_PACK8 ? held : plain;
+    const uint64_t xbytes = L.op == DELTA_OP_EMBEDDING ? (uint64_t)rows * 8 : L.pack && L.op != DELTA_OP_PACK8 && L.op != DELTA_OP_RMSNORM ? held : plain;
     if (c->tensors[L.x].bytes != xbytes)
         return fail(c, DELTA_ERR_INVALID, "layer %u: input tensor %u has %llu bytes, layer needs %llu", i, L.x,
                     (unsigned long long)c->tensors[L.x].bytes, (unsigned long long)xbytes);
@@ -879,6 +895,54 @@ static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint3
         const char *why = delta::embedding_check(L.w, L.scale, rows, L.Cin, L.Cout);
         if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
         ybytes = (uint64_t)rows * L.Cout * es;
+        break;
+    }
+    case DELTA_OP_RMSNORM: {
+        if (L.Cout != L.Cin) return fail(c, DELTA_ERR_INVALID, "layer %u: root-mean-square normalisation keeps the shape", i);
+        if (!(L.eps >= 0.f)) return fail(c, DELTA_ERR_INVALID, "layer %u: eps must be >= 0", i);
+        const char *why = delta::rmsnorm_check(L.scale, rows, L.Cin);
+        if (!why && L.pack) why = delta::pack8_check(c->arena, c->arena, rows, L.Cin, (int)L.pack);
+        if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
+        if (L.res != DELTA_NO_TENSOR && c->tensors[L.res].bytes != plain)
+            return fail(c, DELTA_ERR_INVALID, "layer %u: residual tensor %u has the wrong size", i, L.res);
+        if ((L.res != DELTA_NO_TENSOR) != (L.y2 != DELTA_NO_TENSOR) || (L.y2 != DELTA_NO_TENSOR && c->tensors[L.y2].bytes != plain))
+            return fail(c, DELTA_ERR_INVALID, "layer %u: y2 must be a tensor with the bytes of x exactly when there is a residual", i);
+        if ((L.pack != 0) != (L.y3 != DELTA_NO_TENSOR) || (L.pack && c->tensors[L.y3].bytes != held))
+            return fail(c, DELTA_ERR_INVALID, "layer %u: y3 must be a tensor with the checkpoint's bytes exactly when pack names a format", i);
+        ybytes = plain;
+        break;
+    }
+    case DELTA_OP_ROTARY: {
+        if (L.Cout != L.Cin) return fail(c, DELTA_ERR_INVALID, "layer %u: rotary positions keep the shape", i);
+        if (L.res == DELTA_NO_TENSOR || c->tensors[L.res].bytes % ((uint64_t)rows * 8))
+            return fail(c, DELTA_ERR_INVALID, "layer %u: positions must hold 1 to 8 int64 values for each row", i);
+        const uint64_t axes = c->tensors[L.res].bytes / ((uint64_t)rows * 8);
+        const char *why = delta::rotary_check(L.scale, rows, L.Cin, L.R, L.S, axes > 8 ? 9 : (long long)axes);
+        if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
+        if (L.y2 != DELTA_NO_TENSOR || L.y3 != DELTA_NO_TENSOR) return fail(c, DELTA_ERR_INVALID, "layer %u: rotary positions have one output", i);
+        ybytes = plain;
+        break;
+    }
+    case DELTA_OP_ATTENTION_PACKED: {
+        if (L.res == DELTA_NO_TENSOR || c->tensors[L.res].bytes % 8)
+            return fail(c, DELTA_ERR_INVALID, "layer %u: offsets must hold one int64 value more than there are sequences", i);
+        const char *why = delta::packed_attention_check(rows, (long long)(c->tensors[L.res].bytes / 8) - 1, L.Cin, L.Cout, L.R, L.S, bf16);
+        if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
+        if (L.y2 != DELTA_NO_TENSOR && c->tensors[L.y2].bytes != (uint64_t)rows * L.R * 4)
+            return fail(c, DELTA_ERR_INVALID, "layer %u: y2, the log-sum-exp, must hold R values for each row", i);
+        if (L.y3 != DELTA_NO_TENSOR) return fail(c, DELTA_ERR_INVALID, "layer %u: attention has no third output", i);
+        ybytes = (uint64_t)rows * L.Cout * es;
+        break;
+    }
+    case DELTA_OP_LOGPROB: {
+        const char *why = delta::logprob_check(rows, L.Cin, L.Cout);
+        if (why) return fail(c, DELTA_ERR_INVALID, "layer %u: %s", i, why);
+        if (L.res == DELTA_NO_TENSOR || c->tensors[L.res].bytes != (uint64_t)rows * 8)
+            return fail(c, DELTA_ERR_INVALID, "layer %u: token ids must hold one int64 value for each row", i);
+        if ((L.Cout != 0) != (L.y2 != DELTA_NO_TENSOR) || (L.Cout != 0) != (L.y3 != DELTA_NO_TENSOR) ||
+            (L.Cout && (c->tensors[L.y2].bytes != (uint64_t)rows * L.Cout * 4 || c->tensors[L.y3].bytes != (uint64_t)rows * L.Cout * 8)))
+            return fail(c, DELTA_ERR_INVALID, "layer %u: y2 and y3 must hold Cout fp32 and int64 values for each row exactly when Cout > 0", i);
+        ybytes = (uint64_t)rows * 12;
         break;
     }
     case DELTA_OP_BATCHNORM:
@@ -990,6 +1054,28 @@ static delta_status claim_output(delta_ctx *c, Tensor &ty) {
     return DELTA_OK;
 }
 
+// The same for all outputs of an operator that may have several: y, and at[0], at[1] the addresses of y2 and y3 (null: none).  Where one finds no
+// room, those that were not resident are not resident again: nothing has been computed.
+static delta_status claim_outputs(delta_ctx *c, const delta_layer_desc &L, unsigned char *(&at)[2]) {
+    const uint32_t ids[3] = {L.y, L.y2, L.y3};
+    bool fresh[3] = {false, false, false};
+    for (int j = 0; j < 3; ++j) {
+        if (j && ids[j] == DELTA_NO_TENSOR) continue;
+        Tensor &t = c->tensors[ids[j]];
+        fresh[j] = !t.resident;
+        const delta_status r = claim_output(c, t);
+        if (r != DELTA_OK) {
+            const std::string why = c->err;
+            for (int k = 0; k < j; ++k)
+                if (fresh[k]) (void)drop_block(c, c->tensors[ids[k]]);
+            c->err = why;
+            return r;
+        }
+        if (j) at[j - 1] = c->arena + t.offset;
+    }
+    return DELTA_OK;
+}
+
 // How many of the layers from `i` on are one pass over the elements: a batch normalisation, the add of its result, the ReLU of that, each
 // of which reads what the one before it leaves; or an add and its ReLU.  1: the layer goes by itself.
 static uint32_t elementwise_run(const delta_layer_desc *layers, uint32_t n_layers, uint32_t i) {
@@ -1041,6 +1127,10 @@ delta_status delta_recompute_segment(delta_ctx *c, const delta_layer_desc *layer
         if (L.res != DELTA_NO_TENSOR && !c->tensors[L.res].resident && !will_exist[L.res])
             return fail(c, DELTA_ERR_STATE, "layer %u: second input tensor %u is not resident", i, L.res);
         will_exist[L.y] = 1;
+        if (decoder_op(L)) {
+            if (L.y2 != DELTA_NO_TENSOR) will_exist[L.y2] = 1;
+            if (L.y3 != DELTA_NO_TENSOR) will_exist[L.y3] = 1;
+        }
     }
     // Pass 2: allocate outputs and launch, in order, on the compute stream.
     for (uint32_t i = 0; i < n_layers; ++i) {
@@ -1076,7 +1166,12 @@ delta_status delta_recompute_segment(delta_ctx *c, const delta_layer_desc *layer
         Tensor &ty = c->tensors[L.y];
         if ((r = compute_uses(c, tx)) != DELTA_OK) return r;
         if (L.res != DELTA_NO_TENSOR && (r = compute_uses(c, c->tensors[L.res])) != DELTA_OK) return r;
-        if ((r = claim_output(c, ty)) != DELTA_OK) return r;
+        unsigned char *further[2] = {nullptr, nullptr};
+        if (decoder_op(L)) {
+            if ((r = claim_outputs(c, L, further)) != DELTA_OK) return r;
+        } else if ((r = claim_output(c, ty)) != DELTA_OK) {
+            return r;
+        }
         unsigned char *xp = c->arena + tx.offset, *yp = c->arena + ty.offset;
         unsigned char *rp = L.res != DELTA_NO_TENSOR ? c->arena + c->tensors[L.res].offset : nullptr;
         const long long rows = (long long)L.N * L.H * L.W;
@@ -1142,6 +1237,23 @@ delta_status delta_recompute_segment(delta_ctx *c, const delta_layer_desc *layer
             break;
         case DELTA_OP_EMBEDDING:
             HIP_TRY(c, delta::launch_embedding(xp, L.w, L.scale, yp, rows, L.Cin, L.Cout, L.dtype == DELTA_DTYPE_BF16, c->stream[S_COMPUTE]));
+            break;
+        case DELTA_OP_RMSNORM:
+            HIP_TRY(c, delta::launch_rmsnorm(xp, rp, yp, further[0], further[1], L.scale, rows, L.Cin, L.eps, L.dtype == DELTA_DTYPE_BF16, (int)L.pack,
+                                             c->stream[S_COMPUTE]));
+            break;
+        case DELTA_OP_ROTARY:
+            HIP_TRY(c, delta::launch_rotary(xp, rp, yp, L.scale, rows, L.Cin, L.R, L.S, (int)(c->tensors[L.res].bytes / ((uint64_t)rows * 8)),
+                                            L.flags & DELTA_ROTARY_PAIRS, 0, L.dtype == DELTA_DTYPE_BF16, c->stream[S_COMPUTE]));
+            break;
+        case DELTA_OP_ATTENTION_PACKED:
+            HIP_TRY(c, delta::launch_packed_attention(xp, rp, yp, reinterpret_cast<float *>(further[0]), rows, (long long)(c->tensors[L.res].bytes / 8) - 1,
+                                                      L.Cin, L.Cout, L.R, L.S, L.flags & DELTA_ATTENTION_CAUSAL, 1, c->stream[S_COMPUTE]));
+            break;
+        case DELTA_OP_LOGPROB:
+            HIP_TRY(c, delta::launch_logprob(xp, rp, reinterpret_cast<float *>(yp), reinterpret_cast<float *>(further[0]),
+                                             reinterpret_cast<long long *>(further[1]), rows, L.Cin, L.Cout, L.dtype == DELTA_DTYPE_BF16,
+                                             c->stream[S_COMPUTE]));
             break;
         case DELTA_OP_LAYERNORM:
             HIP_TRY(c, delta::launch_layernorm(xp, yp, L.scale, L.shift, (long long)L.N * L.H * L.W, L.Cin, L.eps,
@@ -1332,7 +1444,7 @@ delta_status need_identity_factors(delta_ctx *c) {
     return DELTA_OK;
 }
 
-enum BwdKind { BK_CONV, BK_DENSE, BK_MAXPOOL, BK_AVGPOOL, BK_LOSS, BK_STEM, BK_BATCHNORM, BK_RELU, BK_LAYERNORM, BK_EMBEDDING };
+enum BwdKind { BK_CONV, BK_DENSE, BK_MAXPOOL, BK_AVGPOOL, BK_LOSS, BK_STEM, BK_BATCHNORM, BK_RELU, BK_LAYERNORM, BK_EMBEDDING, BK_DECODER };
 
 bool is_stem(const delta_layer_desc &L) {
     return L.op == DELTA_OP_CONV && L.dtype == DELTA_DTYPE_BF16 && L.R == 7 && L.S == 7 && L.stride == 2 && L.pad == 3 &&
@@ -1349,6 +1461,7 @@ BwdKind bwd_kind(const delta_layer_desc &L) {
     if (L.op == DELTA_OP_RELU) return BK_RELU;
     if (L.op == DELTA_OP_LAYERNORM) return BK_LAYERNORM;
     if (L.op == DELTA_OP_EMBEDDING) return BK_EMBEDDING;
+    if (decoder_op(L)) return BK_DECODER;
     if (is_stem(L)) return BK_STEM;
     if (L.op == DELTA_OP_CONV && L.H == 1 && L.W == 1 && L.R == 1 && L.S == 1 && L.stride == 1 && L.pad == 0 && L.Cout % 64 != 0) return BK_DENSE;
     return BK_CONV;
@@ -1408,6 +1521,54 @@ delta_status prepare_backward_rows(delta_ctx *c, const delta_bwd_desc &D, uint32
     }
     if (D.gw && ((uintptr_t)D.gw & 15)) return fail(c, DELTA_ERR_INVALID, "backward %u: gw misaligned", i);
     if (D.gw && (!D.workspace || ((uintptr_t)D.workspace & 255) || D.workspace_bytes < row_op_workspace_bytes(L)))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: workspace missing, not 256-byte aligned or too small", i);
+    return DELTA_OK;
+}
+
+// A decoder layer's operators.  Workspace: root-mean-square normalisation's for gw, attention's for gx.
+uint64_t decoder_workspace_bytes(const delta_layer_desc &L) {
+    const long long rows = (long long)L.N * L.H * L.W;
+    const uint64_t need = L.op == DELTA_OP_RMSNORM ? delta::rmsnorm_bwd_workspace_bytes(rows, L.Cin)
+                          : L.op == DELTA_OP_ATTENTION_PACKED ? delta::packed_attention_bwd_workspace_bytes(rows, L.R) : 0;
+    return (need + 255) / 256 * 256;
+}
+// What the gradient reads beside gy and gx_add: `n` ids.
+uint32_t decoder_reads(const delta_layer_desc &L, uint32_t (&ids)[4]) {
+    switch (L.op) {
+    case DELTA_OP_RMSNORM: ids[0] = L.res != DELTA_NO_TENSOR ? L.y2 : L.x; return 1;
+    case DELTA_OP_ROTARY: ids[0] = L.res; return 1;
+    case DELTA_OP_ATTENTION_PACKED: ids[0] = L.x; ids[1] = L.res; ids[2] = L.y; ids[3] = L.y2; return 4;
+    default: ids[0] = L.x; ids[1] = L.res; ids[2] = L.y; return 3;
+    }
+}
+delta_status prepare_backward_decoder(delta_ctx *c, const delta_bwd_desc &D, uint32_t i) {
+    delta::ConvArgs a;
+    delta::PoolArgs pa;
+    uint64_t flops = 0;
+    const delta_layer_desc &L = D.fwd;
+    delta_status r = prepare_layer(c, L, i, a, pa, flops, true);
+    if (r != DELTA_OK) return r;
+    const size_t nt = c->tensors.size();
+    const bool norm = L.op == DELTA_OP_RMSNORM;
+    if (D.mask_gx || D.gy_masked) return fail(c, DELTA_ERR_INVALID, "backward %u: this operator has no masks", i);
+    if (D.gy >= nt || c->tensors[D.gy].bytes != c->tensors[L.y].bytes || D.gpre != D.gy)
+        return fail(c, DELTA_ERR_INVALID, "backward %u: gy must have the bytes of y and gpre must be gy", i);
+    if (!norm && (D.gx == DELTA_NO_TENSOR || D.gx_add != DELTA_NO_TENSOR || D.gw))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: this operator has gx alone (gx_add, gw unused)", i);
+    if (D.gx == DELTA_NO_TENSOR && (!D.gw || D.gx_add != DELTA_NO_TENSOR))
+        return fail(c, DELTA_ERR_INVALID, "backward %u: nothing to compute, or gx_add without gx", i);
+    if (L.op == DELTA_OP_ATTENTION_PACKED && L.y2 == DELTA_NO_TENSOR)
+        return fail(c, DELTA_ERR_INVALID, "backward %u: attention's gradient needs the log-sum-exp (y2)", i);
+    if (D.gx != DELTA_NO_TENSOR) {
+        if (D.gx >= nt || c->tensors[D.gx].bytes != input_bytes(L) || D.gx == L.x || D.gx == L.res || D.gx == L.y || D.gx == L.y2 || D.gx == L.y3 ||
+            D.gx == D.gy)
+            return fail(c, DELTA_ERR_INVALID, "backward %u: gx must be another tensor with the bytes of x", i);
+        if (D.gx_add != DELTA_NO_TENSOR && (D.gx_add >= nt || c->tensors[D.gx_add].bytes != input_bytes(L) || D.gx_add == D.gx))
+            return fail(c, DELTA_ERR_INVALID, "backward %u: gx_add must be another tensor with the bytes of gx", i);
+    }
+    if (D.gw && ((uintptr_t)D.gw & 15)) return fail(c, DELTA_ERR_INVALID, "backward %u: gw misaligned", i);
+    if ((D.gw || L.op == DELTA_OP_ATTENTION_PACKED) &&
+        (!D.workspace || ((uintptr_t)D.workspace & 255) || D.workspace_bytes < decoder_workspace_bytes(L)))
         return fail(c, DELTA_ERR_INVALID, "backward %u: workspace missing, not 256-byte aligned or too small", i);
     return DELTA_OK;
 }
@@ -1713,6 +1874,7 @@ delta_status delta_backward_workspace(delta_ctx *c, const delta_layer_desc *laye
         *out_bytes = row_op_workspace_bytes(*layer);
         return DELTA_OK;
     }
+    if (decoder_op(*layer)) { *out_bytes = decoder_workspace_bytes(*layer); return DELTA_OK; }
     if (layer->op != DELTA_OP_CONV) { *out_bytes = 0; return DELTA_OK; }
     if (is_stem(*layer)) { *out_bytes = delta::stem_wgrad_workspace_bytes(a); return DELTA_OK; }
     as_stride_1(*layer, a);
@@ -1756,6 +1918,18 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
             if ((r = prepare_backward_rows(c, D, i)) != DELTA_OK) return r;
             if (!there(D.gy)) return fail(c, DELTA_ERR_STATE, "backward %u: gy tensor %u is not resident", i, D.gy);
             if (!there(D.fwd.x)) return fail(c, DELTA_ERR_STATE, "backward %u: x tensor %u is not resident", i, D.fwd.x);
+            if (D.gx_add != DELTA_NO_TENSOR && !there(D.gx_add))
+                return fail(c, DELTA_ERR_STATE, "backward %u: gx_add tensor %u is not resident", i, D.gx_add);
+            if (D.gx != DELTA_NO_TENSOR) will_exist[D.gx] = 1;
+            continue;
+        }
+        if (kind == BK_DECODER) {
+            if ((r = prepare_backward_decoder(c, D, i)) != DELTA_OK) return r;
+            uint32_t reads[4];
+            const uint32_t n_reads = decoder_reads(D.fwd, reads);
+            if (!there(D.gy)) return fail(c, DELTA_ERR_STATE, "backward %u: gy tensor %u is not resident", i, D.gy);
+            for (uint32_t j = 0; j < n_reads; ++j)
+                if (!there(reads[j])) return fail(c, DELTA_ERR_STATE, "backward %u: tensor %u is not resident", i, reads[j]);
             if (D.gx_add != DELTA_NO_TENSOR && !there(D.gx_add))
                 return fail(c, DELTA_ERR_STATE, "backward %u: gx_add tensor %u is not resident", i, D.gx_add);
             if (D.gx != DELTA_NO_TENSOR) will_exist[D.gx] = 1;
@@ -1841,6 +2015,53 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
             else
                 HIP_TRY(c, delta::launch_embedding_bwd(c->arena + tx.offset, c->arena + tgy.offset, L.scale, static_cast<float *>(D.gw), rows, L.Cin,
                                                        L.Cout, bf16, sums, need, s));
+            c->st.recompute_launches += 1;
+            continue;
+        }
+        if (kind == BK_DECODER) {
+            if ((r = prepare_backward_decoder(c, D, i)) != DELTA_OK) return r;
+            uint32_t reads[4];
+            const uint32_t n_reads = decoder_reads(L, reads);
+            const unsigned char *in[4] = {nullptr, nullptr, nullptr, nullptr}, *addp = nullptr;
+            for (uint32_t j = 0; j < n_reads; ++j) {
+                if ((r = compute_uses(c, c->tensors[reads[j]])) != DELTA_OK) return r;
+                in[j] = c->arena + c->tensors[reads[j]].offset;
+            }
+            if ((r = compute_uses(c, c->tensors[D.gy])) != DELTA_OK) return r;
+            const unsigned char *gyp = c->arena + c->tensors[D.gy].offset;
+            if (D.gx_add != DELTA_NO_TENSOR) {
+                if ((r = compute_uses(c, c->tensors[D.gx_add])) != DELTA_OK) return r;
+                addp = c->arena + c->tensors[D.gx_add].offset;
+            }
+            unsigned char *gxp = nullptr;
+            if (D.gx != DELTA_NO_TENSOR) {
+                if ((r = compute_writes(c, c->tensors[D.gx])) != DELTA_OK) return r;
+                gxp = c->arena + c->tensors[D.gx].offset;
+            }
+            // as for the row operators: the end of the workspace
+            const uint64_t need = D.gw || L.op == DELTA_OP_ATTENTION_PACKED ? decoder_workspace_bytes(L) : 0;
+            unsigned char *work = need ? static_cast<unsigned char *>(D.workspace) + ((D.workspace_bytes - need) & ~(uint64_t)255) : nullptr;
+            if (need && aux_holds(c, work, need) && (r = join_aux(c)) != DELTA_OK) return r;
+            const long long rows = (long long)L.N * L.H * L.W;
+            const int bf16 = L.dtype == DELTA_DTYPE_BF16;
+            switch (L.op) {
+            case DELTA_OP_RMSNORM:
+                HIP_TRY(c, delta::launch_rmsnorm_bwd(in[0], gyp, addp, gxp, L.scale, static_cast<float *>(D.gw), rows, L.Cin, L.eps, bf16, work, need, s));
+                break;
+            case DELTA_OP_ROTARY:
+                HIP_TRY(c, delta::launch_rotary(gyp, in[0], gxp, L.scale, rows, L.Cin, L.R, L.S, (int)(c->tensors[L.res].bytes / ((uint64_t)rows * 8)),
+                                                L.flags & DELTA_ROTARY_PAIRS, 1, bf16, s));
+                break;
+            case DELTA_OP_ATTENTION_PACKED:
+                HIP_TRY(c, delta::launch_packed_attention_bwd(in[0], in[1], in[2], reinterpret_cast<const float *>(in[3]), gyp, gxp, rows,
+                                                              (long long)(c->tensors[L.res].bytes / 8) - 1, L.Cin, L.Cout, L.R, L.S,
+                                                              L.flags & DELTA_ATTENTION_CAUSAL, bf16, work, need, s));
+                break;
+            default:
+                HIP_TRY(c, delta::launch_logprob_bwd(in[0], in[1], reinterpret_cast<const float *>(in[2]), reinterpret_cast<const float *>(gyp), gxp, rows,
+                                                     L.Cin, bf16, s));
+                break;
+            }
             c->st.recompute_launches += 1;
             continue;
         }
@@ -2105,6 +2326,10 @@ delta_status delta_layer_kernel(delta_ctx *c, const delta_layer_desc *layer, cha
     case DELTA_OP_PACK8: name = layer->pack == DELTA_PACK_INT8 ? "pack8 int8" : "pack8 e4m3"; break;
     case DELTA_OP_UNPACK8: name = layer->pack == DELTA_PACK_INT8 ? "unpack8 int8" : "unpack8 e4m3"; break;
     case DELTA_OP_EMBEDDING: name = layer->dtype == DELTA_DTYPE_BF16 ? "embedding bf16" : "embedding f32"; break;
+    case DELTA_OP_RMSNORM: name = layer->dtype == DELTA_DTYPE_BF16 ? "rmsnorm bf16" : "rmsnorm f32"; break;
+    case DELTA_OP_ROTARY: name = layer->dtype == DELTA_DTYPE_BF16 ? "rotary bf16" : "rotary f32"; break;
+    case DELTA_OP_ATTENTION_PACKED: name = layer->Cout / layer->R == 64 ? "packed_attention bf16, heads of 64" : "packed_attention bf16, heads of 128"; break;
+    case DELTA_OP_LOGPROB: name = layer->dtype == DELTA_DTYPE_BF16 ? "logprob bf16" : "logprob f32"; break;
     case DELTA_OP_BATCHNORM: name = "batchnorm (batch statistics) bf16: stats + finalize + one pass (with an add and ReLU that follow)"; break;
     case DELTA_OP_RELU: name = "relu bf16"; break;
     case DELTA_OP_ADD: name = "add bf16"; break;
@@ -2132,6 +2357,12 @@ delta_status delta_backward_kernel(delta_ctx *c, const delta_bwd_desc *desc, cha
         if ((r = prepare_backward_rows(c, D, 0)) != DELTA_OK) return r;
         const char *from = L.pack == DELTA_PACK_INT8 ? " from int8" : L.pack == DELTA_PACK_E4M3 ? " from e4m3" : "";
         snprintf(out, (size_t)cap, "%s%s%s", D.gx == DELTA_NO_TENSOR ? "gw: " : D.gw ? "gx, gw: " : "gx: ", kind == BK_LAYERNORM ? "layernorm" : "embedding", from);
+        return DELTA_OK;
+    }
+    if (kind == BK_DECODER) {
+        if ((r = prepare_backward_decoder(c, D, 0)) != DELTA_OK) return r;
+        const char *name = L.op == DELTA_OP_RMSNORM ? "rmsnorm" : L.op == DELTA_OP_ROTARY ? "rotary" : L.op == DELTA_OP_LOGPROB ? "logprob" : "packed_attention";
+        snprintf(out, (size_t)cap, "%s%s", D.gx == DELTA_NO_TENSOR ? "gw: " : D.gw ? "gx, gw: " : "gx: ", name);
         return DELTA_OK;
     }
     if (kind != BK_CONV) {

@@ -174,6 +174,28 @@ hipError_t launch_embedding(const void *id, const void *w, const float *scale, v
 size_t embedding_bwd_workspace_bytes(long long n, int V, int C);
 hipError_t launch_embedding_bwd(const void *id, const void *gy, const float *scale, float *gw, long long n, int V, int C, int bf16, void *workspace,
                                 size_t workspace_bytes, hipStream_t stream);
+// rmsnorm.hip: root-mean-square normalisation, residual in front, checkpoint of the result beside it; its gradients
+const char *rmsnorm_check(const float *gamma, long long rows, int C);
+hipError_t launch_rmsnorm(const void *x, const void *res, void *y, void *sum, void *held, const float *gamma, long long rows, int C, float eps, int bf16,
+                          int fmt, hipStream_t stream);
+size_t rmsnorm_bwd_workspace_bytes(long long rows, int C);
+hipError_t launch_rmsnorm_bwd(const void *s, const void *gy, const void *add, void *gx, const float *gamma, float *gw, long long rows, int C, float eps,
+                              int bf16, void *workspace, size_t workspace_bytes, hipStream_t stream);
+// rotary.hip: rotary positions with several axes (backward: by the negative angle)
+const char *rotary_check(const float *freq, long long rows, int channels, int heads, int rest, long long axes);
+hipError_t launch_rotary(const void *x, const void *pos, void *y, const float *freq, long long rows, int channels, int heads, int rest, int axes, int pairs,
+                         int backward, int bf16, hipStream_t stream);
+// packed_attention.hip, packed_attention_bwd.hip: attention over packed sequences with grouped heads, and its gradients
+const char *packed_attention_check(long long M, long long seqs, int Cin, int Cout, int heads, int kv, int bf16);
+hipError_t launch_packed_attention(const void *x, const void *off, void *y, float *lse, long long M, long long seqs, int Cin, int Cout, int heads, int kv,
+                                   int causal, int bf16, hipStream_t stream);
+size_t packed_attention_bwd_workspace_bytes(long long M, int heads);
+hipError_t launch_packed_attention_bwd(const void *x, const void *off, const void *y, const float *lse, const void *gy, void *gx, long long M, long long seqs,
+                                       int Cin, int Cout, int heads, int kv, int causal, int bf16, void *workspace, size_t workspace_bytes, hipStream_t stream);
+// logprob.hip: log probabilities of given tokens, entropy, log-sum-exp, most likely tokens; gradients
+const char *logprob_check(long long rows, int V, int K);
+hipError_t launch_logprob(const void *z, const void *id, float *y, float *best, long long *which, long long rows, int V, int K, int bf16, hipStream_t stream);
+hipError_t launch_logprob_bwd(const void *z, const void *id, const float *y, const float *gy, void *gz, long long rows, int V, int bf16, hipStream_t stream);
 // opgranular_ops.hip: training-mode batch normalisation over [M, C] (bf16), ReLU, residual add
 const char *bn_train_check(const void *x, const void *y, const float *gamma, const float *beta, long long M, int C,
                            int bf16);

@@ -1,0 +1,300 @@
+// Log probabilities of given tokens over a vocabulary of any size for gfx950, bf16 and fp32, with the distribution's entropy, its log-sum-exp and its most
+// likely tokens, and the gradients.
+//   lse = log sum_j exp z_j,  lp = z[id] - lse,  H = lse - sum_j p_j z_j,  p_j = exp(z_j - lse)
+//   gz_j = g_lp ([j = id] - p_j) - g_H p_j (z_j - lse + H) + g_lse p_j
+// One pass over the logits: a thread keeps the largest value m so far, s = sum exp(z - m) and w = sum (m - z) exp(z - m), and scales s and w where m
+// grows; threads meet through LDS.  lp = (z - m) - log s and H = log s + w / s: no difference of large numbers.
+//   A value of -infinity has no weight (z - m is held above -1e30, so that 0 * infinity is not formed).  Where no value has any, lp = lse = -infinity and
+//   H = 0, and the row's gradient is zero.  NaN, or +infinity, makes the row NaN.
+//
+// Alternatives.  A wavefront keeps its K best (value, index) sorted over its lanes, best first; a value enters if it is not at most the K-th (in a
+// wavefront's order of reading a later equal one has the higher index and stays out), by a shift of the lanes behind its place.  The wavefronts' lists meet
+// in LDS.  Order: value (a NaN above all, -0 as 0), of equal ones the lowest index: exact, from the logits' own bits.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.hpp"
+#include "rows.hpp"
+
+namespace delta {
+namespace lpr {
+
+using rows::f32x4;
+using rows::u32x4;
+
+constexpr int kMostK = 64;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Args {
+    const unsigned char *z;                              // [rows][V]
+    const long long *id;
+    float *y;                                            // [3][rows]: lp, H, lse
+    float *best;                                         // [rows][K]
+    long long *which;
+    const float *gy;                                     // [3][rows]
+    unsigned char *gz;
+    uint32_t rows, V, K;
+};
+
+// Eight neighbouring values from any address of the type: rows of odd length begin anywhere.
+template <typename T> __device__ __forceinline__ void load_any(const unsigned char *p, float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        u32x4 raw;
+        __builtin_memcpy(&raw, p, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(raw[e] << 16);
+            v[2 * e + 1] = __uint_as_float(raw[e] & 0xFFFF0000u);
+        }
+    } else {
+        f32x4 a, b;
+        __builtin_memcpy(&a, p, 16);
+        __builtin_memcpy(&b, p + 16, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    }
+}
+template <typename T> __device__ __forceinline__ float load_one(const unsigned char *p) {
+    if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
+    else return *reinterpret_cast<const float *>(p);
+}
+template <typename T> __device__ __forceinline__ void store_any(unsigned char *p, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        const u32x4 raw = {rows::pack2(v[0], v[1]), rows::pack2(v[2], v[3]), rows::pack2(v[4], v[5]), rows::pack2(v[6], v[7])};
+        __builtin_memcpy(p, &raw, 16);
+    } else {
+        const f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+        __builtin_memcpy(p, &a, 16);
+        __builtin_memcpy(p + 16, &b, 16);
+    }
+}
+template <typename T> __device__ __forceinline__ void store_one(unsigned char *p, float v) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t *>(p) = (uint16_t)rows::pack2(v, v);
+    else *reinterpret_cast<float *>(p) = v;
+}
+
+// The running sums of some values.  m is finite from the start (the lowest fp32 number: rows of just that value are uniform), so that no difference of
+// infinities is formed; a NaN reaches s through 2^t.
+struct Sums {
+    float m, s, w;
+    __device__ __forceinline__ void none() { m = -3.402823466e38f; s = w = 0.f; }
+    // from m to a larger one
+    __device__ __forceinline__ void raise(float to) {
+        const float d = fmaxf(m - to, -1e30f), f = __builtin_amdgcn_exp2f(d * kLog2e);
+        w = f * (w - s * d);
+        s *= f;
+        m = to;
+    }
+    __device__ __forceinline__ void add(float v) {
+        const float d = v - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+        s += e;
+        w = __builtin_fmaf(-fmaxf(d, -1e30f), e, w);
+    }
+    __device__ __forceinline__ void join(Sums o) {
+        const float to = fmaxf(m, o.m);
+        raise(to);
+        o.raise(to);
+        s += o.s;
+        w += o.w;
+    }
+};
+
+// A value's place in the order, as a whole number: NaN above all, -0 as 0.
+__device__ __forceinline__ int32_t order_of(float v) {
+    if (v != v) return 0x7FC00000;
+    const int32_t b = (int32_t)__float_as_uint(v + 0.f);
+    return b < 0 ? b ^ 0x7FFFFFFF : b;
+}
+__device__ __forceinline__ float value_of(int32_t o) { return __uint_as_float((uint32_t)(o < 0 ? o ^ 0x7FFFFFFF : o)); }
+// Value, then index: the larger one goes first.
+__device__ __forceinline__ unsigned long long key_of(float v, uint32_t j) {
+    return (unsigned long long)((uint32_t)order_of(v) ^ 0x80000000u) << 32 | (0xFFFFFFFFu - j);
+}
+__device__ __forceinline__ unsigned long long lane_of(unsigned long long v, int lane) {
+    return (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+// A wavefront's K best keys, lane i the i-th; zero where there is none yet (no value has that key).
+struct Best {
+    unsigned long long key;
+    unsigned long long least;                            // the K-th, the same in all lanes
+    __device__ __forceinline__ void none() { key = least = 0; }
+    __device__ __forceinline__ void insert(unsigned long long k, uint32_t K) {     // k the same in all lanes, above `least`
+        const uint32_t lane = threadIdx.x & 63;
+        const int at = __builtin_popcountll(__ballot(key > k));
+        const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)key, 1), hi = (uint32_t)__shfl_up((int)(key >> 32), 1);
+        if ((int)lane == at) key = k;
+        else if ((int)lane > at) key = (unsigned long long)hi << 32 | lo;
+        least = lane_of(key, (int)K - 1);
+    }
+    // The value of each lane that has one (`there`), at the lane's index.
+    __device__ __forceinline__ void offer(float v, uint32_t j, bool there, uint32_t K) {
+        const unsigned long long k = there ? key_of(v, j) : 0;
+        unsigned long long todo = __ballot(k > least);
+        while (todo) {
+            const int lane = __builtin_ctzll(todo);
+            insert(lane_of(k, lane), K);
+            todo &= todo - 1;
+            todo &= __ballot(k > least);
+        }
+    }
+};
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(1024) void forward_kernel(Args a) {
+    constexpr uint32_t kEs = (uint32_t)sizeof(T);
+    extern __shared__ __align__(16) unsigned long long keys[];                     // [wavefronts][K]
+    __shared__ Sums part[16];
+    const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), waves = blockDim.x >> 6;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const long long id = a.id[row];
+        if (id < 0 || id >= a.V) {                       // no token
+            if (threadIdx.x < 3) a.y[(uint64_t)threadIdx.x * a.rows + row] = 0.f;
+            if (TOP && threadIdx.x < a.K) {
+                a.best[(uint64_t)row * a.K + threadIdx.x] = 0.f;
+                a.which[(uint64_t)row * a.K + threadIdx.x] = -1;
+            }
+            continue;
+        }
+        const unsigned char *z = a.z + (uint64_t)row * a.V * kEs;
+        Sums u;
+        u.none();
+        Best top;
+        top.none();
+        const uint32_t pieces = a.V / 8;
+        for (uint32_t p0 = wave * 64; p0 < pieces; p0 += blockDim.x) {
+            const uint32_t p = p0 + lane;
+            const bool there = p < pieces;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = -__builtin_inff();
+            if (there) load_any<T>(z + (uint64_t)p * 8 * kEs, v);
+            float mx = v[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
+            if (mx > u.m) u.raise(mx);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u.add(v[e]);
+            if (TOP)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top.offer(v[e], p * 8 + e, there, a.K);
+        }
+        if (wave == waves - 1) {                         // what is left of the row: its highest indices
+            const uint32_t j = pieces * 8 + lane;
+            const bool there = j < a.V;
+            const float v = there ? load_one<T>(z + (uint64_t)j * kEs) : -__builtin_inff();
+            if (v > u.m) u.raise(v);
+            u.add(v);
+            if (TOP) top.offer(v, j, there, a.K);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            Sums o;
+            o.m = __shfl_xor(u.m, d); o.s = __shfl_xor(u.s, d); o.w = __shfl_xor(u.w, d);
+            u.join(o);
+        }
+        if (lane == 0) part[wave] = u;
+        if (TOP && lane < a.K) keys[wave * a.K + lane] = top.key;
+        __syncthreads();
+        u = part[0];
+        for (uint32_t w = 1; w < waves; ++w) u.join(part[w]);
+        const float logs = __builtin_amdgcn_logf(u.s) * kLn2;                      // -infinity where nothing has weight
+        auto lp = [&](float v) { return (v - u.m) - logs; };
+        if (threadIdx.x == 0) {
+            const float v = load_one<T>(z + (uint64_t)id * kEs);
+            const bool none = u.s == 0.f;
+            a.y[row] = none ? -__builtin_inff() : lp(v);
+            a.y[(uint64_t)a.rows + row] = none ? 0.f : logs + u.w / u.s;
+            a.y[(uint64_t)2 * a.rows + row] = u.m + logs;
+        }
+        if (TOP) {
+            const uint32_t n = waves * a.K;
+            for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+                const unsigned long long k = keys[i];
+                uint32_t rank = 0;
+                for (uint32_t o = 0; o < n; ++o) rank += keys[o] > k;
+                if (rank < a.K && k) {
+                    const float v = value_of((int32_t)((uint32_t)(k >> 32) ^ 0x80000000u));
+                    a.best[(uint64_t)row * a.K + rank] = u.s == 0.f ? -__builtin_inff() : lp(v);
+                    a.which[(uint64_t)row * a.K + rank] = (long long)(0xFFFFFFFFu - (uint32_t)k);
+                }
+            }
+        }
+        __syncthreads();                                 // the parts and the lists are read
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void backward_kernel(Args a, uint32_t chunks) {
+    constexpr uint32_t kEs = (uint32_t)sizeof(T), kChunk = 256 * 8;
+    const uint64_t n = (uint64_t)a.rows * chunks;
+    for (uint64_t b = blockIdx.x; b < n; b += gridDim.x) {
+        const uint32_t row = (uint32_t)(b / chunks), j = (uint32_t)(b - (uint64_t)row * chunks) * kChunk + threadIdx.x * 8;
+        if (j >= a.V) continue;
+        const long long id = a.id[row];
+        const float lse = a.y[(uint64_t)2 * a.rows + row];
+        const bool live = id >= 0 && id < a.V && lse != -__builtin_inff();
+        const float H = a.y[(uint64_t)a.rows + row], g1 = a.gy[row], g2 = a.gy[(uint64_t)a.rows + row], g3 = a.gy[(uint64_t)2 * a.rows + row];
+        const uint64_t at = ((uint64_t)row * a.V + j) * kEs;
+        const bool whole = j + 8 <= a.V;
+        float v[8], o[8];
+        if (live) {
+            if (whole) load_any<T>(a.z + at, v);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = j + e < a.V ? load_one<T>(a.z + at + e * kEs) : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float g = 0.f;
+            if (live) {
+                const float d = v[e] - lse, p = __builtin_amdgcn_exp2f(d * kLog2e);
+                if (p != 0.f) g = p * ((g3 - g1) - g2 * (d + H));
+                if (j + e == (uint32_t)id) g += g1;
+            }
+            o[e] = g;
+        }
+        if (whole) store_any<T>(a.gz + at, o);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + e < a.V) store_one<T>(a.gz + at + e * kEs, o[e]);
+    }
+}
+
+}  // namespace lpr
+
+const char *logprob_check(long long rows, int V, int K) {
+    if (V <= 0 || rows <= 0 || rows > 0x7FFFFFFFLL) return "log probabilities take 1 to 2147483647 rows";
+    if (K < 0 || K > lpr::kMostK || K > V) return "log probabilities give 0 to 64 alternatives, no more than there are tokens";
+    return nullptr;
+}
+
+// y: [3][rows]; best, which: [rows][K], null with K = 0.
+hipError_t launch_logprob(const void *z, const void *id, float *y, float *best, long long *which, long long rows, int V, int K, int bf16, hipStream_t stream) {
+    if (!z || !id || !y || logprob_check(rows, V, K) || (K && (!best || !which))) return hipErrorInvalidValue;
+    lpr::Args a = {};
+    a.z = static_cast<const unsigned char *>(z); a.id = static_cast<const long long *>(id); a.y = y; a.best = best; a.which = which;
+    a.rows = (uint32_t)rows; a.V = (uint32_t)V; a.K = (uint32_t)K;
+    const uint32_t waves = V >= 16 * 1024 ? 16 : V >= 4096 ? 4 : 1;
+    auto run = [&](auto kernel) { kernel<<<dim3(a.rows < 65536u ? a.rows : 65536u), dim3(waves * 64), waves * a.K * sizeof(unsigned long long), stream>>>(a); };
+    if (bf16) { if (K) run(lpr::forward_kernel<rows::bf16, true>); else run(lpr::forward_kernel<rows::bf16, false>); }
+    else { if (K) run(lpr::forward_kernel<float, true>); else run(lpr::forward_kernel<float, false>); }
+    return hipGetLastError();
+}
+
+// y: what the forward pass left; gy: [3][rows].
+hipError_t launch_logprob_bwd(const void *z, const void *id, const float *y, const float *gy, void *gz, long long rows, int V, int bf16, hipStream_t stream) {
+    if (!z || !id || !y || !gy || !gz || logprob_check(rows, V, 0)) return hipErrorInvalidValue;
+    lpr::Args a = {};
+    a.z = static_cast<const unsigned char *>(z); a.id = static_cast<const long long *>(id); a.y = const_cast<float *>(y); a.gy = gy;
+    a.gz = static_cast<unsigned char *>(gz); a.rows = (uint32_t)rows; a.V = (uint32_t)V;
+    const uint32_t chunks = (a.V + 2047) / 2048;
+    const uint64_t n = (uint64_t)a.rows * chunks;
+    auto run = [&](auto kernel) { kernel<<<dim3((unsigned)(n < (1u << 20) ? n : 1u << 20)), dim3(256), 0, stream>>>(a, chunks); };
+    if (bf16) run(lpr::backward_kernel<rows::bf16>);
+    else run(lpr::backward_kernel<float>);
+    return hipGetLastError();
+}
+
+}  // namespace delta

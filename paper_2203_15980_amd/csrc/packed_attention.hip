@@ -1,0 +1,179 @@
+// Attention over packed sequences (forward) for gfx950: ctx = softmax(q k^T / sqrt D) v per query head and sequence, causal or not, R query heads over S key
+// heads (head h reads key head h / (R / S)), D = 64 or 128, bf16; and the scores' log-sum-exp, which the gradients read.
+//
+// Layout.  x [M, (R + 2 S) D]: R heads of queries, S of keys, S of values; y [M, R D]; lse [R, M].  Sequence i is rows off[i] .. off[i+1] - 1; rows of
+// no sequence are zero in y and lse (packed_attention.hpp: how a workgroup finds its rows).
+//
+// A workgroup takes one head and 32 queries a wavefront; K and V of its sequence stream through LDS in blocks of 64 keys, two buffers, the block after
+// next on its way in registers.  Everything is computed transposed, as in attention.hip: S^T = K Q^T, so that a lane owns a query and its softmax statistics are
+// the lane's own; O^T += V^T P^T with P straight from the accumulators.  Running maximum and sum in fp32; P is rounded to bf16 before it multiplies V.
+// Causal: a workgroup ends at its last query's block, a wavefront skips the blocks behind its own last query, and only blocks that a border crosses are masked.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.hpp"
+#include "packed_attention.hpp"
+
+namespace delta {
+namespace pat {
+
+constexpr int kBlock = 64;                               // keys to a block
+
+template <int D> constexpr int kBuffer = 2 * kBlock * kPitch<D>;                   // K and V of a block
+
+template <int D, int W, bool CAUSAL>
+__global__ __launch_bounds__(W * 64) void forward_kernel(Args a) {
+    constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
+    const int head = (int)(blockIdx.x % (unsigned)a.heads), slot = a.slots - 1 - (int)(blockIdx.x / (unsigned)a.heads);
+    Rows r;
+    if (!find_rows<Q>(a, slot, r)) return;
+    const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
+    const int q0 = r.tile * Q;
+    unsigned char *yb = a.y + (size_t)r.start * out_pitch + (size_t)head * D * 2;
+    float *lse = a.lse ? a.lse + (size_t)head * a.M + r.start : nullptr;
+    if (r.alone) {
+        const int n = r.len - q0 < Q ? r.len - q0 : Q;
+        zero_rows(yb + (size_t)q0 * out_pitch, out_pitch, n, D * 2);
+        if (lse && (int)threadIdx.x < n) lse[q0 + threadIdx.x] = 0.f;
+        return;
+    }
+    const unsigned char *xb = a.x + (size_t)r.start * pitch;
+    const int kh = head / (a.heads / a.kv);
+    const unsigned char *kb = xb + (size_t)(a.heads + kh) * D * 2, *vb = kb + (size_t)a.kv * D * 2;
+    const int w0 = q0 + 32 * wave, q = w0 + l32;
+    const bool there = q < r.len;
+    bf16x8 qf[KS];
+    {
+        const unsigned char *p = xb + (size_t)(there ? q : r.len - 1) * pitch + (size_t)head * D * 2 + half * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p + s * 32));
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int t = 0; t < DB; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+    float m_run = -__builtin_inff(), l_run = 0.f;        // l_run: this half-wave's share of the sum
+    const int keys = CAUSAL && q0 + Q < r.len ? q0 + Q : r.len, blocks = (keys + kBlock - 1) / kBlock;
+    const int limit = CAUSAL && q + 1 < r.len ? q + 1 : r.len;                     // the lane's keys
+    Tile<D, kBlock, W * 64> tk, tv;
+    auto fetch = [&](int b) {
+        tk.fetch(kb, pitch, b * kBlock, r.len);
+        tv.fetch(vb, pitch, b * kBlock, r.len);
+    };
+    auto stage = [&](int b) {
+        unsigned char *at = smem + (b & 1) * kBuffer<D>;
+        tk.store(at);
+        tv.store(at + kBlock * kPitch<D>);
+    };
+    fetch(0);
+    stage(0);
+    fetch(1);
+    __syncthreads();
+    for (int b = 0; b < blocks; ++b) {
+        if (b + 1 < blocks) stage(b + 1);                // that buffer's last readers passed the barrier below
+        fetch(b + 2);
+        const unsigned char *ks = smem + (b & 1) * kBuffer<D>, *vs = ks + kBlock * kPitch<D>;
+        const int k0 = b * kBlock;
+        if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
+            f32x16 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) s[t] = mfma(rows_of<D>(ks, 32 * t, k), qf[k], s[t]);
+            }
+            if (__builtin_expect(k0 + kBlock > (CAUSAL ? (w0 + 1 < r.len ? w0 + 1 : r.len) : r.len), 0)) {
+                const int lim = limit - k0 - 4 * half;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[t][e] = 32 * t + row_of(e) < lim ? s[t][e] : -__builtin_inff();
+                asm volatile("" ::: "memory");           // keeps the masked path a separate block
+            }
+            float mx = -__builtin_inff();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[t][e]);
+            const float m_new = fmaxf(m_run, halves_max(mx) * a.scale_log2e);      // finite: key 0 is every query's
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);             // 0 on the first block
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int t = 0; t < DB; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], a.scale_log2e, -m_new));
+                    sum += s[t][e];
+                }
+                l_run += sum;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x8 p = as_operand(s[t], j);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d] = mfma(columns_of<D>(vs, 32 * t + 16 * j, d), p, o[d]);
+                }
+            }
+        }
+        __syncthreads();                                 // buffer b % 2 is free; block b + 1 is visible
+    }
+    l_run = rows::halves(l_run);
+    if (!there) return;
+    store_column<DB>(yb + (size_t)q * out_pitch, o, 1.0f / l_run);
+    if (lse && !half) lse[q] = (m_run + __builtin_amdgcn_logf(l_run)) * 0.6931471805599453f;
+}
+
+template <int D, int W, bool CAUSAL>
+static hipError_t forward(Args a, hipStream_t stream) {
+    constexpr int kLds = 2 * kBuffer<D>;
+    if (kLds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&forward_kernel<D, W, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (e != hipSuccess) return e;
+    }
+    a.slots = slots_of(a.M, a.seqs, W * 32);
+    forward_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * 64), kLds, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace pat
+
+// x [M, (heads + 2 kv) D], `seqs` sequences.
+const char *packed_attention_check(long long M, long long seqs, int Cin, int Cout, int heads, int kv, int bf16) {
+    if (!bf16) return "attention is bf16 only";
+    if (heads <= 0 || kv <= 0 || heads % kv) return "attention needs R query heads, a multiple of S key heads";
+    if (Cout % heads || (Cout / heads != 64 && Cout / heads != 128) || (long long)Cout / heads * (heads + 2LL * kv) != Cin)
+        return "attention needs heads of 64 or 128 channels, Cout = R D, Cin = (R + 2 S) D";
+    if (M <= 0 || M > 0x7FFFFF00LL) return "attention takes 1 to 2147483392 rows";
+    if (seqs < 1 || seqs > 0x3FFFFFFFLL) return "offsets must hold one int64 value more than there are sequences";
+    // threads of a launch: 128 queries or keys to 256 threads, and a workgroup to each sequence and each end
+    if ((M / 128 + seqs + 2) * heads * 256 > 0x7FFFFFFFLL) return "too many rows, sequences and heads in one launch";
+    return nullptr;
+}
+
+static pat::Args packed_attention_args(const void *x, const void *off, void *y, float *lse, long long M, long long seqs, int Cout, int heads, int kv) {
+    pat::Args a = {};
+    a.x = static_cast<const unsigned char *>(x); a.off = static_cast<const long long *>(off); a.y = static_cast<unsigned char *>(y); a.lse = lse;
+    a.M = (int)M; a.seqs = (int)seqs; a.heads = heads; a.kv = kv;
+    a.scale = 1.0f / sqrtf((float)(Cout / heads));
+    a.scale_log2e = a.scale * 1.4426950408889634f;
+    return a;
+}
+
+hipError_t launch_packed_attention(const void *x, const void *off, void *y, float *lse, long long M, long long seqs, int Cin, int Cout, int heads, int kv,
+                                   int causal, int bf16, hipStream_t stream) {
+    if (!x || !off || !y || packed_attention_check(M, seqs, Cin, Cout, heads, kv, bf16)) return hipErrorInvalidValue;
+    const pat::Args a = packed_attention_args(x, off, y, lse, M, seqs, Cout, heads, kv);
+    if (Cout / heads == 64) return causal ? pat::forward<64, 4, true>(a, stream) : pat::forward<64, 4, false>(a, stream);
+    return causal ? pat::forward<128, 4, true>(a, stream) : pat::forward<128, 4, false>(a, stream);
+}
+
+}  // namespace delta

@@ -1,0 +1,278 @@
+// The gradients of attention over packed sequences (packed_attention.hip) for gfx950.  With p = exp(s - lse), s = q k^T / sqrt D:
+//   delta = sum over a row's channels of ctx gctx,  dp = gctx v^T,  ds = p (dp - delta)
+//   gq = ds k / sqrt D,  gk = ds^T q / sqrt D,  gv = p^T gctx, gk and gv summed over the query heads of their key head
+// Two launches and no atomics: one owns queries (delta, which it leaves for the other, and gq), one owns keys and walks through the queries of all its heads
+// in order, so that a gradient's bits depend on its inputs alone.  Scores are formed twice: 7 products where 5 would do, against 32-bit sums of gq that would
+// have to meet across workgroups.
+//   gq: as the forward kernel, a lane owns a query: S^T = K Q^T, dP^T = V gO^T, gQ^T += K^T dS^T.
+//   gk, gv: a lane owns a key: S = Q K^T, dP = gO V^T, gV^T += gO^T P, gK^T += Q^T dS; queries and their gradients come through LDS.
+// p and ds are rounded to bf16 before they multiply; all sums are fp32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.hpp"
+#include "packed_attention.hpp"
+
+namespace delta {
+namespace pat {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kStep = 64;                                // keys (of gq's kernel) or queries (of the other's) to a block
+
+template <int D> constexpr int kPair = 2 * kStep * kPitch<D>;                      // two tiles
+
+template <int D, int W, bool CAUSAL>
+__global__ __launch_bounds__(W * 64) void gq_kernel(Args a) {
+    constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
+    const int head = (int)(blockIdx.x % (unsigned)a.heads), slot = a.slots - 1 - (int)(blockIdx.x / (unsigned)a.heads);
+    Rows r;
+    if (!find_rows<Q>(a, slot, r)) return;
+    const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
+    const int q0 = r.tile * Q;
+    unsigned char *gxb = a.gx + (size_t)r.start * pitch + (size_t)head * D * 2;
+    if (r.alone) {
+        zero_rows(gxb + (size_t)q0 * pitch, pitch, r.len - q0 < Q ? r.len - q0 : Q, D * 2);
+        return;
+    }
+    const unsigned char *xb = a.x + (size_t)r.start * pitch;
+    const int kh = head / (a.heads / a.kv);
+    const unsigned char *kb = xb + (size_t)(a.heads + kh) * D * 2, *vb = kb + (size_t)a.kv * D * 2;
+    const int w0 = q0 + 32 * wave, q = w0 + l32;
+    const bool there = q < r.len;
+    const int row = there ? q : r.len - 1;
+    bf16x8 qf[KS], gf[KS];
+    float delta = 0.f;
+    {
+        const unsigned char *p = xb + (size_t)row * pitch + (size_t)head * D * 2 + half * 16;
+        const size_t at = ((size_t)r.start + row) * out_pitch + (size_t)head * D * 2 + half * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p + s * 32));
+            rows::Eight<rows::bf16> g, y;
+            g.load(a.gy + at + s * 32);
+            y.load(a.y + at + s * 32);
+            gf[s] = __builtin_bit_cast(bf16x8, g.raw);
+            float u[8], v[8];
+            g.to(u);
+            y.to(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta += u[e] * v[e];
+        }
+    }
+    delta = rows::halves(delta);
+    const size_t stat = (size_t)head * a.M + r.start + row;
+    const float lse2 = a.lse[stat] * kLog2e;
+    if (there && !half) a.delta[stat] = delta;
+    f32x16 g[DB];
+#pragma unroll
+    for (int t = 0; t < DB; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) g[t][e] = 0.f;
+    const int keys = CAUSAL && q0 + Q < r.len ? q0 + Q : r.len, blocks = (keys + kStep - 1) / kStep;
+    const int limit = CAUSAL && q + 1 < r.len ? q + 1 : r.len;
+    Tile<D, kStep, W * 64> tk, tv;
+    auto fetch = [&](int b) {
+        tk.fetch(kb, pitch, b * kStep, r.len);
+        tv.fetch(vb, pitch, b * kStep, r.len);
+    };
+    auto stage = [&](int b) {
+        unsigned char *at = smem + (b & 1) * kPair<D>;
+        tk.store(at);
+        tv.store(at + kStep * kPitch<D>);
+    };
+    fetch(0);
+    stage(0);
+    fetch(1);
+    __syncthreads();
+    for (int b = 0; b < blocks; ++b) {
+        if (b + 1 < blocks) stage(b + 1);
+        fetch(b + 2);
+        const unsigned char *ks = smem + (b & 1) * kPair<D>, *vs = ks + kStep * kPitch<D>;
+        const int k0 = b * kStep;
+        if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
+            const bool border = k0 + kStep > (CAUSAL ? (w0 + 1 < r.len ? w0 + 1 : r.len) : r.len);
+            const int lim = border ? limit - k0 - 4 * half : kStep;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x16 s, dp;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    s = mfma(rows_of<D>(ks, 32 * t, k), qf[k], s);
+                    dp = mfma(rows_of<D>(vs, 32 * t, k), gf[k], dp);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2e, -lse2));
+                    s[e] = p * (dp[e] - delta);
+                }
+                if (__builtin_expect(border, 0)) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = 32 * t + row_of(e) < lim ? s[e] : 0.f;
+                    asm volatile("" ::: "memory");
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x8 ds = as_operand(s, j);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) g[d] = mfma(columns_of<D>(ks, 32 * t + 16 * j, d), ds, g[d]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (there) store_column<DB>(gxb + (size_t)q * pitch, g, a.scale);
+}
+
+template <int D, int W, bool CAUSAL>
+__global__ __launch_bounds__(W * 64) void gkv_kernel(Args a) {
+    constexpr int K = W * 32, KS = D / 16, DB = D / 32;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(16) float stats[2][2][kStep];   // of a block's queries: log-sum-exp (log2), delta
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
+    const int kh = (int)(blockIdx.x % (unsigned)a.kv), slot = (int)(blockIdx.x / (unsigned)a.kv);      // first keys first: causal, they have the most queries
+    Rows r;
+    if (!find_rows<K>(a, slot, r)) return;
+    const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
+    const int first = r.tile * K, group = a.heads / a.kv;
+    unsigned char *gkb = a.gx + (size_t)r.start * pitch + (size_t)(a.heads + kh) * D * 2, *gvb = gkb + (size_t)a.kv * D * 2;
+    if (r.alone) {
+        const int n = r.len - first < K ? r.len - first : K;
+        zero_rows(gkb + (size_t)first * pitch, pitch, n, D * 2);
+        zero_rows(gvb + (size_t)first * pitch, pitch, n, D * 2);
+        return;
+    }
+    const unsigned char *xb = a.x + (size_t)r.start * pitch;
+    const int w0 = first + 32 * wave, key = w0 + l32;
+    const bool there = key < r.len;
+    bf16x8 kf[KS], vf[KS];
+    {
+        const unsigned char *p = xb + (size_t)(there ? key : r.len - 1) * pitch + (size_t)(a.heads + kh) * D * 2 + half * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p + s * 32));
+            vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p + (size_t)a.kv * D * 2 + s * 32));
+        }
+    }
+    f32x16 gk[DB], gv[DB];
+#pragma unroll
+    for (int t = 0; t < DB; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) gk[t][e] = gv[t][e] = 0.f;
+    const int begin = CAUSAL ? first / kStep : 0, per = (r.len + kStep - 1) / kStep - begin, blocks = per * group;
+    Tile<D, kStep, W * 64> tq, tg;
+    float st = 0.f;                                      // the thread's statistic of the block on its way: log-sum-exp (threads 0 .. 63), delta (64 .. 127)
+    auto fetch = [&](int b) {
+        if (b >= blocks) return;
+        const int head = kh * group + b / per, at = (begin + b % per) * kStep;
+        tq.fetch(xb + (size_t)head * D * 2, pitch, at, r.len);
+        tg.fetch(a.gy + (size_t)r.start * out_pitch + (size_t)head * D * 2, out_pitch, at, r.len);
+        const int q = at + ((int)threadIdx.x & 63);
+        if (threadIdx.x < 64) st = q < r.len ? a.lse[(size_t)head * a.M + r.start + q] * kLog2e : __builtin_inff();    // p = 0 behind the last query
+        else if (threadIdx.x < 128) st = q < r.len ? a.delta[(size_t)head * a.M + r.start + q] : 0.f;
+    };
+    auto stage = [&](int b) {
+        unsigned char *at = smem + (b & 1) * kPair<D>;
+        tq.store(at);
+        tg.store(at + kStep * kPitch<D>);
+        if (threadIdx.x < 128) stats[b & 1][threadIdx.x >> 6][threadIdx.x & 63] = st;
+    };
+    fetch(0);
+    stage(0);
+    fetch(1);
+    __syncthreads();
+    for (int b = 0; b < blocks; ++b) {
+        if (b + 1 < blocks) stage(b + 1);
+        fetch(b + 2);
+        const unsigned char *qs = smem + (b & 1) * kPair<D>, *gs = qs + kStep * kPitch<D>;
+        const int at = (begin + b % per) * kStep;
+        if (w0 < r.len && (!CAUSAL || at + kStep - 1 >= w0)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x16 s, dp;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    s = mfma(rows_of<D>(qs, 32 * t, k), kf[k], s);
+                    dp = mfma(rows_of<D>(gs, 32 * t, k), vf[k], dp);
+                }
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[b & 1][0][32 * t + 8 * e4 + 4 * half]);
+                    const f32x4 dl = *reinterpret_cast<const f32x4 *>(&stats[b & 1][1][32 * t + 8 * e4 + 4 * half]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * e4 + e], a.scale_log2e, -l[e]));
+                        s[4 * e4 + e] = p;
+                        dp[4 * e4 + e] = p * (dp[4 * e4 + e] - dl[e]);
+                    }
+                }
+                if (CAUSAL && __builtin_expect(at + 32 * t < w0 + 31, 0)) {
+                    const int from = key - at - 32 * t - 4 * half;                 // the first row of the product that sees this key
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        s[e] = row_of(e) >= from ? s[e] : 0.f;
+                        dp[e] = row_of(e) >= from ? dp[e] : 0.f;
+                    }
+                    asm volatile("" ::: "memory");
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x8 p = as_operand(s, j), ds = as_operand(dp, j);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        gv[d] = mfma(columns_of<D>(gs, 32 * t + 16 * j, d), p, gv[d]);
+                        gk[d] = mfma(columns_of<D>(qs, 32 * t + 16 * j, d), ds, gk[d]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (!there) return;
+    store_column<DB>(gkb + (size_t)key * pitch, gk, a.scale);
+    store_column<DB>(gvb + (size_t)key * pitch, gv, 1.0f);
+}
+
+template <int D, int W, bool CAUSAL>
+static hipError_t backward(Args a, hipStream_t stream) {
+    constexpr int kLds = 2 * kPair<D>;
+    if (kLds > 64 * 1024) {
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&gq_kernel<D, W, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (e == hipSuccess)
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(&gkv_kernel<D, W, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (e != hipSuccess) return e;
+    }
+    a.slots = slots_of(a.M, a.seqs, W * 32);
+    gq_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * 64), kLds, stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    gkv_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.kv), dim3(W * 64), kLds, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace pat
+
+size_t packed_attention_bwd_workspace_bytes(long long M, int heads) { return (size_t)M * heads * sizeof(float); }
+
+// y, lse: what the forward pass left; gy as y; gx as x, all of it written (rows of no sequence with zeros).
+hipError_t launch_packed_attention_bwd(const void *x, const void *off, const void *y, const float *lse, const void *gy, void *gx, long long M, long long seqs,
+                                       int Cin, int Cout, int heads, int kv, int causal, int bf16, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!x || !off || !y || !lse || !gy || !gx || packed_attention_check(M, seqs, Cin, Cout, heads, kv, bf16)) return hipErrorInvalidValue;
+    if (!workspace || workspace_bytes < packed_attention_bwd_workspace_bytes(M, heads)) return hipErrorInvalidValue;
+    pat::Args a = {};
+    a.x = static_cast<const unsigned char *>(x); a.off = static_cast<const long long *>(off);
+    a.y = static_cast<unsigned char *>(const_cast<void *>(y)); a.lse = const_cast<float *>(lse);
+    a.gy = static_cast<const unsigned char *>(gy); a.gx = static_cast<unsigned char *>(gx); a.delta = static_cast<float *>(workspace);
+    a.M = (int)M; a.seqs = (int)seqs; a.heads = heads; a.kv = kv;
+    a.scale = 1.0f / sqrtf((float)(Cout / heads));
+    a.scale_log2e = a.scale * pat::kLog2e;
+    if (Cout / heads == 64) return causal ? pat::backward<64, 4, true>(a, stream) : pat::backward<64, 4, false>(a, stream);
+    return causal ? pat::backward<128, 4, true>(a, stream) : pat::backward<128, 4, false>(a, stream);
+}
+
+}  // namespace delta
