@@ -7,9 +7,14 @@
 //   A value of -infinity has no weight (z - m is held above -1e30, so that 0 * infinity is not formed).  Where no value has any, lp = lse = -infinity and
 //   H = 0, and the row's gradient is zero.  NaN, or +infinity, makes the row NaN.
 //
-// Alternatives.  A wavefront keeps its K best (value, index) sorted over its lanes, best first; a value enters if it is not at most the K-th (in a
-// wavefront's order of reading a later equal one has the higher index and stays out), by a shift of the lanes behind its place.  The wavefronts' lists meet
-// in LDS.  Order: value (a NaN above all, -0 as 0), of equal ones the lowest index: exact, from the logits' own bits.
+// Alternatives.  Of 64 groups of threads the K-th largest group maximum is a value that K logits reach at least; the threads whose own maximum reaches it read
+// their logits again and put those that do into LDS (about 64 log(64 / (64 - K)), 24 with K = 20), and each finds its place by counting the larger ones.
+// Where more than 1024 do (long runs of equal logits) or fewer than K groups hold anything, or the row holds a NaN or +infinity, a sorted list over a
+// wavefront's lanes takes the logits one by one instead.  Order: value (a NaN above all, -0 as 0), of equal ones the lowest index: exact, from the logits'
+// own bits.
+//
+// Bound by memory where there are many rows: 4096 x 131072 in bf16 (1.07 GB) forward 208 to 234 us (4.6 to 5.2 TB/s), gradient 395 to 430 us (2.15 GB, 5.0 to
+// 5.4 TB/s).  333 x 50001 in fp32 with 5 alternatives 24 us (67 MB), gradient 21 us; one row of 30522 with 20 alternatives 8.6 to 10.6 us: latency.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -37,23 +42,29 @@ struct Args {
 };
 
 // Eight neighbouring values from any address of the type: rows of odd length begin anywhere.
-template <typename T> __device__ __forceinline__ void load_any(const unsigned char *p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        u32x4 raw;
-        __builtin_memcpy(&raw, p, 16);
+template <typename T> struct Raw;
+template <> struct Raw<rows::bf16> {
+    u32x4 raw;
+    __device__ __forceinline__ void load(const unsigned char *p) { __builtin_memcpy(&raw, p, 16); }
+    __device__ __forceinline__ void to(float (&v)[8]) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             v[2 * e] = __uint_as_float(raw[e] << 16);
             v[2 * e + 1] = __uint_as_float(raw[e] & 0xFFFF0000u);
         }
-    } else {
-        f32x4 a, b;
+    }
+};
+template <> struct Raw<float> {
+    f32x4 a, b;
+    __device__ __forceinline__ void load(const unsigned char *p) {
         __builtin_memcpy(&a, p, 16);
         __builtin_memcpy(&b, p + 16, 16);
+    }
+    __device__ __forceinline__ void to(float (&v)[8]) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
     }
-}
+};
 template <typename T> __device__ __forceinline__ float load_one(const unsigned char *p) {
     if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16);
     else return *reinterpret_cast<const float *>(p);
@@ -89,13 +100,6 @@ struct Sums {
         const float d = v - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
         s += e;
         w = __builtin_fmaf(-fmaxf(d, -1e30f), e, w);
-    }
-    __device__ __forceinline__ void join(Sums o) {
-        const float to = fmaxf(m, o.m);
-        raise(to);
-        o.raise(to);
-        s += o.s;
-        w += o.w;
     }
 };
 
@@ -140,13 +144,91 @@ struct Best {
     }
 };
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));           // no canonicalising of values that are as they came from memory
+    return r;
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, rows::dpp<0xB1>(v));
+    v = fmaxf(v, rows::dpp<0x4E>(v));
+    v = fmaxf(v, rows::dpp<0x141>(v));
+    v = fmaxf(v, rows::dpp<0x140>(v));
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// The thread's pieces of eight values, threadIdx.x + k * blockDim.x, three in flight: f(values, piece).  One copy of f and moves of what is in flight: a launch over few
+// rows waits for its instructions to come from memory too.  With it and with eight copies of f in loops of four pieces: 1 x 30522 in fp32 with 20 alternatives 12.0 and 14.9 us, 333 x 50001
+// with 5 28.9 and 37.9 us, 4096 x 131072 in bf16 231 and 267 us.
+template <typename T>
+struct Pieces {
+    Raw<T> ahead[3];
+    uint32_t n;
+    __device__ __forceinline__ void fetch(const unsigned char *z, uint32_t pieces) {     // the first three
+        n = pieces;
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (threadIdx.x + k * blockDim.x < n) ahead[k].load(z + (uint64_t)(threadIdx.x + k * blockDim.x) * 8 * sizeof(T));
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(const unsigned char *z, F &&f) {                // after fetch
+        const uint64_t step = blockDim.x;
+#pragma unroll 1
+        for (uint64_t p = threadIdx.x; p < n; p += step) {
+            float v[8];
+            ahead[0].to(v);
+            ahead[0] = ahead[1];
+            ahead[1] = ahead[2];
+            if (p + 3 * step < n) ahead[2].load(z + (p + 3 * step) * 8 * sizeof(T));
+            f(v, (uint32_t)p);
+        }
+    }
+};
+
+constexpr uint32_t kMostThere = 1024;                    // candidates in LDS
+
+// Lists over the lanes: each wavefront's over its share of the row, then the first one's over all lists.  keys: [wavefronts][64].
+template <typename T>
+__device__ __forceinline__ void sorted_best(const unsigned char *z, uint32_t V, uint32_t K, unsigned long long *keys, uint32_t wave, uint32_t waves, Best &top) {
+    const uint32_t lane = threadIdx.x & 63;
+    top.none();
+    for (uint32_t j0 = wave * 64; j0 < V; j0 += waves * 64) {
+        const uint32_t j = j0 + lane;
+        top.offer(j < V ? load_one<T>(z + (uint64_t)j * sizeof(T)) : 0.f, j, j < V, K);
+    }
+    __syncthreads();                                     // what `keys` held is read
+    keys[wave * 64 + lane] = lane < K ? top.key : 0;
+    __syncthreads();
+    if (wave) return;
+    for (uint32_t w = 1; w < waves; ++w) {
+        const unsigned long long k = keys[w * 64 + lane];
+        unsigned long long todo = __ballot(k > top.least);
+        while (todo) {
+            top.insert(lane_of(k, __builtin_ctzll(todo)), K);
+            todo &= todo - 1;
+            todo &= __ballot(k > top.least);
+        }
+    }
+}
+
 template <typename T, bool TOP>
 __global__ __launch_bounds__(1024) void forward_kernel(Args a) {
     constexpr uint32_t kEs = (uint32_t)sizeof(T);
-    extern __shared__ __align__(16) unsigned long long keys[];                     // [wavefronts][K]
-    __shared__ Sums part[16];
+    __shared__ __align__(16) Sums part[16];
+    __shared__ __align__(16) unsigned long long keys[TOP ? kMostThere : 1];        // also [wavefronts][64]
+    __shared__ float most[64];
+    __shared__ uint32_t place[64];
+    __shared__ uint32_t found;
     const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), waves = blockDim.x >> 6;
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const unsigned char *z = a.z + (uint64_t)row * a.V * kEs;
+        const uint32_t pieces = a.V / 8, rest = pieces * 8 + threadIdx.x;          // the last V % 8 values go to the first threads
+        Pieces<T> in;
+        in.fetch(z, pieces);                             // on their way while the id is looked at
+        const float last = rest < a.V ? load_one<T>(z + (uint64_t)rest * kEs) : -__builtin_inff();
         const long long id = a.id[row];
         if (id < 0 || id >= a.V) {                       // no token
             if (threadIdx.x < 3) a.y[(uint64_t)threadIdx.x * a.rows + row] = 0.f;
@@ -156,71 +238,112 @@ __global__ __launch_bounds__(1024) void forward_kernel(Args a) {
             }
             continue;
         }
-        const unsigned char *z = a.z + (uint64_t)row * a.V * kEs;
+        const float mine = load_one<T>(z + (uint64_t)id * kEs);
         Sums u;
         u.none();
-        Best top;
-        top.none();
-        const uint32_t pieces = a.V / 8;
-        for (uint32_t p0 = wave * 64; p0 < pieces; p0 += blockDim.x) {
-            const uint32_t p = p0 + lane;
-            const bool there = p < pieces;
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = -__builtin_inff();
-            if (there) load_any<T>(z + (uint64_t)p * 8 * kEs, v);
-            float mx = v[0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, v[e]);
+        auto take = [&](const float (&v)[8]) {
+            const float mx = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], u.m));
             if (mx > u.m) u.raise(mx);
 #pragma unroll
             for (int e = 0; e < 8; ++e) u.add(v[e]);
-            if (TOP)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) top.offer(v[e], p * 8 + e, there, a.K);
+        };
+        in.each(z, [&](const float (&v)[8], uint32_t) { take(v); });
+        if (rest < a.V) {
+            if (last > u.m) u.raise(last);
+            u.add(last);
         }
-        if (wave == waves - 1) {                         // what is left of the row: its highest indices
-            const uint32_t j = pieces * 8 + lane;
-            const bool there = j < a.V;
-            const float v = there ? load_one<T>(z + (uint64_t)j * kEs) : -__builtin_inff();
-            if (v > u.m) u.raise(v);
-            u.add(v);
-            if (TOP) top.offer(v, j, there, a.K);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            Sums o;
-            o.m = __shfl_xor(u.m, d); o.s = __shfl_xor(u.s, d); o.w = __shfl_xor(u.w, d);
-            u.join(o);
-        }
+        const float own = u.m;                           // the thread's largest (not of NaN)
+        u.raise(wave_max(u.m));
+        u.s = rows::wave_sum(u.s);
+        u.w = rows::wave_sum(u.w);
         if (lane == 0) part[wave] = u;
-        if (TOP && lane < a.K) keys[wave * a.K + lane] = top.key;
+        if (TOP) {
+            // groups: a row of 16 lanes of 16 wavefronts, a quad of 4, a lane of 1
+            float g = own;
+            if (waves >= 4) {
+                g = fmaxf(g, rows::dpp<0xB1>(g));
+                g = fmaxf(g, rows::dpp<0x4E>(g));
+            }
+            if (waves == 16) {
+                g = fmaxf(g, rows::dpp<0x141>(g));
+                g = fmaxf(g, rows::dpp<0x140>(g));
+            }
+            const uint32_t per = waves;                  // lanes of a group
+            if ((lane & (per - 1)) == 0) most[threadIdx.x / per] = g;
+            if (threadIdx.x < 64) place[threadIdx.x] = 0;
+            if (threadIdx.x == 0) found = 0;
+        }
         __syncthreads();
-        u = part[0];
-        for (uint32_t w = 1; w < waves; ++w) u.join(part[w]);
+        {
+            Sums o = part[lane < waves ? lane : 0];
+            o.raise(wave_max(o.m));
+            u.m = o.m;
+            u.s = rows::wave_sum(lane < waves ? o.s : 0.f);
+            u.w = rows::wave_sum(lane < waves ? o.w : 0.f);
+        }
         const float logs = __builtin_amdgcn_logf(u.s) * kLn2;                      // -infinity where nothing has weight
         auto lp = [&](float v) { return (v - u.m) - logs; };
+        const bool none = u.s == 0.f;
         if (threadIdx.x == 0) {
-            const float v = load_one<T>(z + (uint64_t)id * kEs);
-            const bool none = u.s == 0.f;
-            a.y[row] = none ? -__builtin_inff() : lp(v);
+            a.y[row] = none ? -__builtin_inff() : lp(mine);
             a.y[(uint64_t)a.rows + row] = none ? 0.f : logs + u.w / u.s;
             a.y[(uint64_t)2 * a.rows + row] = u.m + logs;
         }
         if (TOP) {
-            const uint32_t n = waves * a.K;
-            for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-                const unsigned long long k = keys[i];
-                uint32_t rank = 0;
-                for (uint32_t o = 0; o < n; ++o) rank += keys[o] > k;
-                if (rank < a.K && k) {
-                    const float v = value_of((int32_t)((uint32_t)(k >> 32) ^ 0x80000000u));
-                    a.best[(uint64_t)row * a.K + rank] = u.s == 0.f ? -__builtin_inff() : lp(v);
-                    a.which[(uint64_t)row * a.K + rank] = (long long)(0xFFFFFFFFu - (uint32_t)k);
+            auto put = [&](uint32_t at, unsigned long long k) {
+                const float v = value_of((int32_t)((uint32_t)(k >> 32) ^ 0x80000000u));
+                a.best[(uint64_t)row * a.K + at] = none ? -__builtin_inff() : lp(v);
+                a.which[(uint64_t)row * a.K + at] = (long long)(0xFFFFFFFFu - (uint32_t)k);
+            };
+            // the groups' order: each wavefront compares its share of them with all (all 64 in each of 16 wavefronts took 2 us of a row)
+            const float g = most[lane];
+            const int share = 64 / (int)waves;
+            uint32_t above = 0;
+#pragma unroll 4
+            for (int o = (int)wave * share; o < (int)(wave + 1) * share; ++o) {
+                const float h = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(g), o));
+                above += h > g || (h == g && o < (int)lane);
+            }
+            atomicAdd(&place[lane], above);
+            __syncthreads();
+            above = place[lane];
+            const float bar = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(g), __builtin_ctzll(__ballot(above == a.K - 1))));
+            bool listed = u.s == u.s && bar > -3.402823466e38f;                    // the lowest number: fewer than K groups hold anything
+            if (listed) {
+                auto offer = [&](float v, uint32_t j) {
+                    if (v >= bar) {
+                        const uint32_t at = atomicAdd(&found, 1u);
+                        if (at < kMostThere) keys[at] = key_of(v, j);
+                    }
+                };
+                if (own >= bar) {
+                    in.fetch(z, pieces);
+                    in.each(z, [&](const float (&v)[8], uint32_t q) {
+                        if (max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7])) < bar) return;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) offer(v[e], q * 8 + e);
+                    });
+                    if (rest < a.V) offer(last, rest);
                 }
+                __syncthreads();
+                const uint32_t n = found;
+                listed = n <= kMostThere;
+                if (listed)
+                    for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+                        const unsigned long long k = keys[i];
+                        uint32_t rank = 0;
+#pragma unroll 4
+                        for (uint32_t o = 0; o < n; ++o) rank += keys[o] > k;
+                        if (rank < a.K) put(rank, k);
+                    }
+            }
+            if (!listed) {
+                Best top;
+                sorted_best<T>(z, a.V, a.K, keys, wave, waves, top);
+                if (wave == 0 && lane < a.K) put(lane, top.key);
             }
         }
-        __syncthreads();                                 // the parts and the lists are read
+        __syncthreads();                                 // what is in LDS is read
     }
 }
 
@@ -239,7 +362,8 @@ __global__ __launch_bounds__(256) void backward_kernel(Args a, uint32_t chunks) 
         const bool whole = j + 8 <= a.V;
         float v[8], o[8];
         if (live) {
-            if (whole) load_any<T>(a.z + at, v);
+            Raw<T> raw;
+            if (whole) { raw.load(a.z + at); raw.to(v); }
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = j + e < a.V ? load_one<T>(a.z + at + e * kEs) : 0.f;
@@ -277,7 +401,7 @@ hipError_t launch_logprob(const void *z, const void *id, float *y, float *best, 
     a.z = static_cast<const unsigned char *>(z); a.id = static_cast<const long long *>(id); a.y = y; a.best = best; a.which = which;
     a.rows = (uint32_t)rows; a.V = (uint32_t)V; a.K = (uint32_t)K;
     const uint32_t waves = V >= 16 * 1024 ? 16 : V >= 4096 ? 4 : 1;
-    auto run = [&](auto kernel) { kernel<<<dim3(a.rows < 65536u ? a.rows : 65536u), dim3(waves * 64), waves * a.K * sizeof(unsigned long long), stream>>>(a); };
+    auto run = [&](auto kernel) { kernel<<<dim3(a.rows < 65536u ? a.rows : 65536u), dim3(waves * 64), 0, stream>>>(a); };
     if (bf16) { if (K) run(lpr::forward_kernel<rows::bf16, true>); else run(lpr::forward_kernel<rows::bf16, false>); }
     else { if (K) run(lpr::forward_kernel<float, true>); else run(lpr::forward_kernel<float, false>); }
     return hipGetLastError();
