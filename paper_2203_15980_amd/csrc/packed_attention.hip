@@ -18,15 +18,18 @@ namespace delta {
 namespace pat {
 
 constexpr int kBlock = 64;                               // keys to a block
+// The running maximum is raised (and what has been summed scaled) only where a lane's grows by more than this many powers of two: until then weights are up to 2^kLate,
+// which neither fp32 nor bf16 minds, and the quotient is the same.
+constexpr float kLate = 8.f;
 
 template <int D> constexpr int kBuffer = 2 * kBlock * kPitch<D>;                   // K and V of a block
 
 template <int D, int W, bool CAUSAL>
-__global__ __launch_bounds__(W * 64) void forward_kernel(Args a) {
+__global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
     constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
-    const int head = (int)(blockIdx.x % (unsigned)a.heads), slot = a.slots - 1 - (int)(blockIdx.x / (unsigned)a.heads);
+    const int head = head_of((int)(blockIdx.x % (unsigned)a.heads), a.heads), slot = a.slots - 1 - (int)(blockIdx.x / (unsigned)a.heads);
     Rows r;
     if (!find_rows<Q>(a, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
@@ -80,12 +83,13 @@ __global__ __launch_bounds__(W * 64) void forward_kernel(Args a) {
         if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
             f32x16 s[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < KS; ++k) s[t] = mfma(rows_of<D>(ks, 32 * t, k), qf[k], s[t]);
-            }
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) s[t] = mfma(rows_of<D>(ks, 32 * t, k), qf[k], s[t]);
             if (__builtin_expect(k0 + kBlock > (CAUSAL ? (w0 + 1 < r.len ? w0 + 1 : r.len) : r.len), 0)) {
                 const int lim = limit - k0 - 4 * half;
 #pragma unroll
@@ -100,19 +104,21 @@ __global__ __launch_bounds__(W * 64) void forward_kernel(Args a) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[t][e]);
             const float m_new = fmaxf(m_run, halves_max(mx) * a.scale_log2e);      // finite: key 0 is every query's
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);             // 0 on the first block
-            m_run = m_new;
-            l_run *= alpha;
+            if (__any(m_new > m_run + kLate)) {
+                const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);         // 0 on the first block
+                m_run = m_new;
+                l_run *= alpha;
 #pragma unroll
-            for (int t = 0; t < DB; ++t)
+                for (int t = 0; t < DB; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+                    for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+            }
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 float sum = 0.f;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], a.scale_log2e, -m_new));
+                    s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], a.scale_log2e, -m_run));
                     sum += s[t][e];
                 }
                 l_run += sum;

@@ -65,6 +65,9 @@ __device__ __forceinline__ bool find_rows(const Args &a, int slot, Rows &r) {
     return r.tile >= 0 && r.tile * (long long)Q < r.len;
 }
 
+// Consecutive workgroups go to the 8 XCDs in turn, each with an L2 of its own: numbered like this, an XCD's heads are neighbours, which share keys and values.
+__device__ __forceinline__ int head_of(int i, int heads) { return heads % 8 ? i : (i & 7) * (heads >> 3) + (i >> 3); }
+
 // Rows of D bf16 channels in LDS: a pitch of an odd number of 16 bytes, so that neighbouring rows' pieces lie in different banks.
 template <int D> constexpr int kPitch = D * 2 + 16;
 

@@ -22,7 +22,7 @@ constexpr int kStep = 64;                                // keys (of gq's kernel
 template <int D> constexpr int kPair = 2 * kStep * kPitch<D>;                      // two tiles
 
 template <int D, int W, bool CAUSAL>
-__global__ __launch_bounds__(W * 64) void gq_kernel(Args a) {
+__global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
     constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(W * 64) void gq_kernel(Args a) {
 }
 
 template <int D, int W, bool CAUSAL>
-__global__ __launch_bounds__(W * 64) void gkv_kernel(Args a) {
+__global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
     constexpr int K = W * 32, KS = D / 16, DB = D / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) float stats[2][2][kStep];   // of a block's queries: log-sum-exp (log2), delta
