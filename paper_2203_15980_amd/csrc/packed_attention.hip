@@ -4,8 +4,8 @@
 // Layout.  x [M, (R + 2 S) D]: R heads of queries, S of keys, S of values; y [M, R D]; lse [R, M].  Sequence i is rows off[i] .. off[i+1] - 1; rows of
 // no sequence are zero in y and lse (packed_attention.hpp: how a workgroup finds its rows).
 //
-// A workgroup takes one head and 32 queries a wavefront; K and V of its sequence stream through LDS in blocks of 64 keys, two buffers, the block after
-// next on its way in registers.  Everything is computed transposed, as in attention.hip: S^T = K Q^T, so that a lane owns a query and its softmax statistics are
+// A workgroup takes one head and 32 queries a wavefront; K and V of its sequence stream through LDS in blocks of 64 keys, two buffers, the next
+// block on its way from memory straight to LDS.  Everything is computed transposed, as in attention.hip: S^T = K Q^T, so that a lane owns a query and its softmax statistics are
 // the lane's own; O^T += V^T P^T with P straight from the accumulators.  Running maximum and sum in fp32; P is rounded to bf16 before it multiplies V.
 // Causal: a workgroup ends at its last query's block, a wavefront skips the blocks behind its own last query, and only blocks that a border crosses are masked.
 #include <hip/hip_runtime.h>
@@ -22,7 +22,7 @@ constexpr int kBlock = 64;                               // keys to a block
 // which neither fp32 nor bf16 minds, and the quotient is the same.
 constexpr float kLate = 8.f;
 
-template <int D> constexpr int kBuffer = 2 * kBlock * kPitch<D>;                   // K and V of a block
+template <int D> constexpr int kBuffer = 2 * kTile<D>;                             // K and V of a block
 
 template <int D, int W, bool CAUSAL>
 __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
@@ -61,24 +61,20 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
     float m_run = -__builtin_inff(), l_run = 0.f;        // l_run: this half-wave's share of the sum
     const int keys = CAUSAL && q0 + Q < r.len ? q0 + Q : r.len, blocks = (keys + kBlock - 1) / kBlock;
     const int limit = CAUSAL && q + 1 < r.len ? q + 1 : r.len;                     // the lane's keys
-    Tile<D, kBlock, W * 64> tk, tv;
-    auto fetch = [&](int b) {
-        tk.fetch(kb, pitch, b * kBlock, r.len);
-        tv.fetch(vb, pitch, b * kBlock, r.len);
+    const Loader<D, W> loader(wave);
+    const uint32_t lds = lds_of(smem);
+    auto load = [&](int b) {
+        const uint32_t at = lds + (uint32_t)(b & 1) * kBuffer<D>;
+        const size_t from = (size_t)b * kBlock * pitch;
+        loader.load(kb + from, (uint32_t)pitch, r.len - b * kBlock, at);
+        loader.load(vb + from, (uint32_t)pitch, r.len - b * kBlock, at + kTile<D>);
     };
-    auto stage = [&](int b) {
-        unsigned char *at = smem + (b & 1) * kBuffer<D>;
-        tk.store(at);
-        tv.store(at + kBlock * kPitch<D>);
-    };
-    fetch(0);
-    stage(0);
-    fetch(1);
-    __syncthreads();
+    load(0);
     for (int b = 0; b < blocks; ++b) {
-        if (b + 1 < blocks) stage(b + 1);                // that buffer's last readers passed the barrier below
-        fetch(b + 2);
-        const unsigned char *ks = smem + (b & 1) * kBuffer<D>, *vs = ks + kBlock * kPitch<D>;
+        arrived();
+        __syncthreads();                                 // block b is there; block b - 1 is done with
+        if (b + 1 < blocks) load(b + 1);
+        const unsigned char *ks = smem + (b & 1) * kBuffer<D>, *vs = ks + kTile<D>;
         const int k0 = b * kBlock;
         if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
             f32x16 s[2];
@@ -130,7 +126,6 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
                 }
             }
         }
-        __syncthreads();                                 // buffer b % 2 is free; block b + 1 is visible
     }
     l_run = rows::halves(l_run);
     if (!there) return;
@@ -158,6 +153,7 @@ const char *packed_attention_check(long long M, long long seqs, int Cin, int Cou
     if (heads <= 0 || kv <= 0 || heads % kv) return "attention needs R query heads, a multiple of S key heads";
     if (Cout % heads || (Cout / heads != 64 && Cout / heads != 128) || (long long)Cout / heads * (heads + 2LL * kv) != Cin)
         return "attention needs heads of 64 or 128 channels, Cout = R D, Cin = (R + 2 S) D";
+    if (Cin > 1 << 24) return "attention takes rows of at most 16777216 channels";     // 64 of them lie within 32 bits
     if (M <= 0 || M > 0x7FFFFF00LL) return "attention takes 1 to 2147483392 rows";
     if (seqs < 1 || seqs > 0x3FFFFFFFLL) return "offsets must hold one int64 value more than there are sequences";
     // threads of a launch: 128 queries or keys to 256 threads, and a workgroup to each sequence and each end

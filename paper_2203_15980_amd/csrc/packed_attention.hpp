@@ -68,48 +68,56 @@ __device__ __forceinline__ bool find_rows(const Args &a, int slot, Rows &r) {
 // Consecutive workgroups go to the 8 XCDs in turn, each with an L2 of its own: numbered like this, an XCD's heads are neighbours, which share keys and values.
 __device__ __forceinline__ int head_of(int i, int heads) { return heads % 8 ? i : (i & 7) * (heads >> 3) + (i >> 3); }
 
-// Rows of D bf16 channels in LDS: a pitch of an odd number of 16 bytes, so that neighbouring rows' pieces lie in different banks.
-template <int D> constexpr int kPitch = D * 2 + 16;
+// A tile of 64 rows of D bf16 channels in LDS, without padding: piece p (16 bytes) of row r lies at piece p ^ twist(r) of its row, so that both ways of
+// reading it below meet each bank as seldom as can be: 16 lanes that read one piece of 16 rows, and 32 that read 64 bytes of four rows.
+constexpr int kTileRows = 64;
+template <int D> constexpr int kTile = kTileRows * D * 2;
+template <int D>
+__device__ __forceinline__ constexpr int twist(int r) {
+    return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+}
 
-// A tile of 64 rows on its way from memory through registers to LDS, by THREADS threads; rows from `limit` on come as zeros.
-template <int D, int ROWS, int THREADS>
-struct Tile {
-    static constexpr int kPieces = ROWS * (D / 8) / THREADS;
-    static_assert(ROWS * (D / 8) % THREADS == 0, "whole pieces");
-    u32x4 v[kPieces];
-    __device__ __forceinline__ void fetch(const unsigned char *base, size_t pitch, int first, int limit) {
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const int i = (int)threadIdx.x + p * THREADS, r = first + i / (D / 8), seg = i % (D / 8);
-            v[p] = u32x4{0u, 0u, 0u, 0u};
-            if (r < limit) v[p] = *reinterpret_cast<const u32x4 *>(base + (size_t)r * pitch + seg * 16);
-        }
+// Rows of memory straight into such a tile, by W wavefronts: `base` is the tile's first row, at most `rows` of its rows are there (the others come as the last of
+// those).  Whoever reads the tile waits (arrived) and meets the others' barrier first.
+template <int D, int W>
+struct Loader {
+    static constexpr int kRows = 64 * 16 / (D * 2), kTurns = kTileRows / (kRows * W);       // rows of a wavefront's load; loads to a tile
+    static_assert(kTurns * kRows * W == kTileRows && kRows * W % 16 == 0, "the twist of a lane's row is the same in each turn");
+    int row, lds;
+    uint32_t piece;                                      // byte of the row
+    __device__ __forceinline__ Loader(int wave) {
+        const int lane = threadIdx.x & 63;
+        row = wave * kRows + lane / (D / 8);
+        piece = (uint32_t)((lane % (D / 8)) ^ twist<D>(row)) * 16;
+        lds = wave * kRows * D * 2;
     }
-    __device__ __forceinline__ void store(unsigned char *lds) const {
+    __device__ __forceinline__ void load(const unsigned char *base, uint32_t pitch, int rows, uint32_t tile) const {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const int i = (int)threadIdx.x + p * THREADS;
-            *reinterpret_cast<u32x4 *>(lds + (i / (D / 8)) * kPitch<D> + (i % (D / 8)) * 16) = v[p];
+        for (int t = 0; t < kTurns; ++t) {
+            const int r = row + t * kRows * W;
+            load_lds_b128(base, (uint32_t)(r < rows ? r : rows - 1) * pitch + piece, tile + (uint32_t)(lds + t * kRows * W * D * 2));
         }
     }
 };
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_of(const unsigned char *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)p; }
 
-// Operand of a 32 x 32 x 16 product out of LDS: row `row` + lane % 32, channels 16 step + 8 (lane / 32) ..
+// Operand of a 32 x 32 x 16 product out of a tile: row `row` + lane % 32, channels 16 step + 8 (lane / 32) ..
 template <int D>
 __device__ __forceinline__ bf16x8 rows_of(const unsigned char *tile, int row, int step) {
-    const int lane = threadIdx.x & 63;
-    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(tile + (row + (lane & 31)) * kPitch<D> + step * 32 + (lane >> 5) * 16));
+    const int lane = threadIdx.x & 63, r = row + (lane & 31);
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(tile + r * (D * 2) + ((2 * step + (lane >> 5)) ^ twist<D>(lane & 31)) * 16));
 }
-// The same of the transposed tile: channel 32 block + lane % 32, and the eight rows row + 4 (lane / 32) + {0 .. 3, 8 .. 11}: the rows that a lane's eight
-// accumulators of one 32 x 32 product stand for.  ds_read_b64_tr_b16: within 16 lanes, lane j points at row j / 4 and columns 4 (j % 4) .. of a 4 x 16 block and
-// receives column j of its four rows.
+// The same of the transposed tile: channel 32 block + lane % 32, and the eight rows row + 4 (lane / 32) + {0 .. 3, 8 .. 11} (row a multiple of 16): the rows that a
+// lane's eight accumulators of one 32 x 32 product stand for.  ds_read_b64_tr_b16: within 16 lanes, lane j points at row j / 4 and columns 4 (j % 4) .. of a 4 x 16
+// block and receives column j of its four rows.
 template <int D>
 __device__ __forceinline__ bf16x8 columns_of(const unsigned char *tile, int row, int block) {
     typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
-    const int lane = threadIdx.x & 63;
-    const unsigned char *p = tile + (row + 4 * (lane >> 5) + ((lane & 15) >> 2)) * kPitch<D> + (32 * block + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p));
-    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 8 * kPitch<D>));
+    const int lane = threadIdx.x & 63, r = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 4 * block + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+    const unsigned char *p = tile + (row + r) * (D * 2) + (lane & 1) * 8;
+    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + (piece ^ twist<D>(r)) * 16));
+    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 8 * (D * 2) + (piece ^ twist<D>(r + 8)) * 16));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 

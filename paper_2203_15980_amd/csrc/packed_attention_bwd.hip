@@ -19,7 +19,7 @@ namespace pat {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStep = 64;                                // keys (of gq's kernel) or queries (of the other's) to a block
 
-template <int D> constexpr int kPair = 2 * kStep * kPitch<D>;                      // two tiles
+template <int D> constexpr int kPair = 2 * kTile<D>;                               // two tiles
 
 template <int D, int W, bool CAUSAL>
 __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
@@ -72,30 +72,27 @@ __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
         for (int e = 0; e < 16; ++e) g[t][e] = 0.f;
     const int keys = CAUSAL && q0 + Q < r.len ? q0 + Q : r.len, blocks = (keys + kStep - 1) / kStep;
     const int limit = CAUSAL && q + 1 < r.len ? q + 1 : r.len;
-    Tile<D, kStep, W * 64> tk, tv;
-    auto fetch = [&](int b) {
-        tk.fetch(kb, pitch, b * kStep, r.len);
-        tv.fetch(vb, pitch, b * kStep, r.len);
+    const Loader<D, W> loader(wave);
+    const uint32_t lds = lds_of(smem);
+    auto load = [&](int b) {
+        const uint32_t at = lds + (uint32_t)(b & 1) * kPair<D>;
+        const size_t from = (size_t)b * kStep * pitch;
+        loader.load(kb + from, (uint32_t)pitch, r.len - b * kStep, at);
+        loader.load(vb + from, (uint32_t)pitch, r.len - b * kStep, at + kTile<D>);
     };
-    auto stage = [&](int b) {
-        unsigned char *at = smem + (b & 1) * kPair<D>;
-        tk.store(at);
-        tv.store(at + kStep * kPitch<D>);
-    };
-    fetch(0);
-    stage(0);
-    fetch(1);
-    __syncthreads();
+    load(0);
     for (int b = 0; b < blocks; ++b) {
-        if (b + 1 < blocks) stage(b + 1);
-        fetch(b + 2);
-        const unsigned char *ks = smem + (b & 1) * kPair<D>, *vs = ks + kStep * kPitch<D>;
+        arrived();
+        __syncthreads();                                 // block b is there; block b - 1 is done with
+        if (b + 1 < blocks) load(b + 1);
+        const unsigned char *ks = smem + (b & 1) * kPair<D>, *vs = ks + kTile<D>;
         const int k0 = b * kStep;
         if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
             const bool border = k0 + kStep > (CAUSAL ? (w0 + 1 < r.len ? w0 + 1 : r.len) : r.len);
             const int lim = border ? limit - k0 - 4 * half : kStep;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
+                __builtin_amdgcn_sched_barrier(0);       // one tile after the other: both at once do not fit the registers
                 f32x16 s, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.f;
@@ -122,7 +119,6 @@ __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
                 }
             }
         }
-        __syncthreads();
     }
     if (there) store_column<DB>(gxb + (size_t)q * pitch, g, a.scale);
 }
@@ -163,35 +159,30 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) gk[t][e] = gv[t][e] = 0.f;
     const int begin = CAUSAL ? first / kStep : 0, per = (r.len + kStep - 1) / kStep - begin, blocks = per * group;
-    Tile<D, kStep, W * 64> tq, tg;
+    const Loader<D, W> loader(wave);
+    const uint32_t lds = lds_of(smem);
     float st = 0.f;                                      // the thread's statistic of the block on its way: log-sum-exp (threads 0 .. 63), delta (64 .. 127)
-    auto fetch = [&](int b) {
-        if (b >= blocks) return;
+    auto load = [&](int b) {
         const int head = kh * group + b / per, at = (begin + b % per) * kStep;
-        tq.fetch(xb + (size_t)head * D * 2, pitch, at, r.len);
-        tg.fetch(a.gy + (size_t)r.start * out_pitch + (size_t)head * D * 2, out_pitch, at, r.len);
+        const uint32_t to = lds + (uint32_t)(b & 1) * kPair<D>;
+        loader.load(xb + (size_t)at * pitch + (size_t)head * D * 2, (uint32_t)pitch, r.len - at, to);
+        loader.load(a.gy + ((size_t)r.start + at) * out_pitch + (size_t)head * D * 2, (uint32_t)out_pitch, r.len - at, to + kTile<D>);
         const int q = at + ((int)threadIdx.x & 63);
         if (threadIdx.x < 64) st = q < r.len ? a.lse[(size_t)head * a.M + r.start + q] * kLog2e : __builtin_inff();    // p = 0 behind the last query
         else if (threadIdx.x < 128) st = q < r.len ? a.delta[(size_t)head * a.M + r.start + q] : 0.f;
     };
-    auto stage = [&](int b) {
-        unsigned char *at = smem + (b & 1) * kPair<D>;
-        tq.store(at);
-        tg.store(at + kStep * kPitch<D>);
-        if (threadIdx.x < 128) stats[b & 1][threadIdx.x >> 6][threadIdx.x & 63] = st;
-    };
-    fetch(0);
-    stage(0);
-    fetch(1);
-    __syncthreads();
+    load(0);
     for (int b = 0; b < blocks; ++b) {
-        if (b + 1 < blocks) stage(b + 1);
-        fetch(b + 2);
-        const unsigned char *qs = smem + (b & 1) * kPair<D>, *gs = qs + kStep * kPitch<D>;
+        if (threadIdx.x < 128) stats[b & 1][threadIdx.x >> 6][threadIdx.x & 63] = st;
+        arrived();
+        __syncthreads();                                 // block b is there; block b - 1 is done with
+        if (b + 1 < blocks) load(b + 1);
+        const unsigned char *qs = smem + (b & 1) * kPair<D>, *gs = qs + kTile<D>;
         const int at = (begin + b % per) * kStep;
         if (w0 < r.len && (!CAUSAL || at + kStep - 1 >= w0)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
+                __builtin_amdgcn_sched_barrier(0);       // one tile after the other: both at once do not fit the registers
                 f32x16 s, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.f;
@@ -231,7 +222,6 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
                 }
             }
         }
-        __syncthreads();
     }
     if (!there) return;
     store_column<DB>(gkb + (size_t)key * pitch, gk, a.scale);
