@@ -1529,7 +1529,7 @@ delta_status prepare_backward_rows(delta_ctx *c, const delta_bwd_desc &D, uint32
 uint64_t decoder_workspace_bytes(const delta_layer_desc &L) {
     const long long rows = (long long)L.N * L.H * L.W;
     const uint64_t need = L.op == DELTA_OP_RMSNORM ? delta::rmsnorm_bwd_workspace_bytes(rows, L.Cin)
-                          : L.op == DELTA_OP_ATTENTION_PACKED ? delta::packed_attention_bwd_workspace_bytes(rows, L.R) : 0;
+                          : L.op == DELTA_OP_ATTENTION_PACKED ? delta::packed_attention_bwd_workspace_bytes(rows, L.Cout, L.R, L.S) : 0;
     return (need + 255) / 256 * 256;
 }
 // What the gradient reads beside gy and gx_add: `n` ids.

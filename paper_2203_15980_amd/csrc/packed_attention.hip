@@ -136,10 +136,7 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
 template <int D, int W, bool CAUSAL>
 static hipError_t forward(Args a, hipStream_t stream) {
     constexpr int kLds = 2 * kBuffer<D>;
-    if (kLds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&forward_kernel<D, W, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-        if (e != hipSuccess) return e;
-    }
+    static_assert(kLds <= 64 * 1024, "what a launch may ask for without more ado");
     a.slots = slots_of(a.M, a.seqs, W * 32);
     forward_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * 64), kLds, stream>>>(a);
     return hipGetLastError();

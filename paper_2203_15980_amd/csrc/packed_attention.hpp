@@ -24,7 +24,8 @@ struct Args {
     const unsigned char *gy;                             // [M][heads D]
     unsigned char *gx;                                   // as x
     float *delta;                                        // [heads][M], sum over a row's channels of y gy
-    int M, seqs, heads, kv, slots;
+    float *part;                                         // null or [splits][M][2 kv D]: sums of gk and gv over a share of a key head's query heads
+    int M, seqs, heads, kv, slots, splits;
     float scale, scale_log2e;                            // 1 / sqrt(D), times log2 e
 };
 
@@ -68,10 +69,9 @@ __device__ __forceinline__ bool find_rows(const Args &a, int slot, Rows &r) {
 // Consecutive workgroups go to the 8 XCDs in turn, each with an L2 of its own: numbered like this, an XCD's heads are neighbours, which share keys and values.
 __device__ __forceinline__ int head_of(int i, int heads) { return heads % 8 ? i : (i & 7) * (heads >> 3) + (i >> 3); }
 
-// A tile of 64 rows of D bf16 channels in LDS, without padding: piece p (16 bytes) of row r lies at piece p ^ twist(r) of its row, so that both ways of
+// A tile of rows of D bf16 channels in LDS, without padding: piece p (16 bytes) of row r lies at piece p ^ twist(r) of its row, so that both ways of
 // reading it below meet each bank as seldom as can be: 16 lanes that read one piece of 16 rows, and 32 that read 64 bytes of four rows.
-constexpr int kTileRows = 64;
-template <int D> constexpr int kTile = kTileRows * D * 2;
+template <int D, int ROWS = 64> constexpr int kTile = ROWS * D * 2;
 template <int D>
 __device__ __forceinline__ constexpr int twist(int r) {
     return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
@@ -79,10 +79,10 @@ __device__ __forceinline__ constexpr int twist(int r) {
 
 // Rows of memory straight into such a tile, by W wavefronts: `base` is the tile's first row, at most `rows` of its rows are there (the others come as the last of
 // those).  Whoever reads the tile waits (arrived) and meets the others' barrier first.
-template <int D, int W>
+template <int D, int W, int ROWS = 64>
 struct Loader {
-    static constexpr int kRows = 64 * 16 / (D * 2), kTurns = kTileRows / (kRows * W);       // rows of a wavefront's load; loads to a tile
-    static_assert(kTurns * kRows * W == kTileRows && kRows * W % 16 == 0, "the twist of a lane's row is the same in each turn");
+    static constexpr int kRows = 64 * 16 / (D * 2), kTurns = ROWS / (kRows * W);   // rows of a wavefront's load; loads to a tile
+    static_assert(kTurns * kRows * W == ROWS && kRows * W % 16 == 0, "the twist of a lane's row is the same in each turn");
     int row, lds;
     uint32_t piece;                                      // byte of the row
     __device__ __forceinline__ Loader(int wave) {
@@ -149,6 +149,17 @@ __device__ __forceinline__ void store_column(unsigned char *out, const f32x16 (&
             w.y = rows::pack2(o[t][4 * e4 + 2] * by, o[t][4 * e4 + 3] * by);
             *reinterpret_cast<uint2 *>(out + (32 * t + 8 * e4 + 4 * half) * 2) = w;
         }
+}
+
+// The same times `by` in fp32, [channel] from `out` on.
+template <int BLOCKS>
+__device__ __forceinline__ void store_column(float *out, const f32x16 (&o)[BLOCKS], float by) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+            *reinterpret_cast<f32x4 *>(out + 32 * t + 8 * e4 + 4 * half) = f32x4{o[t][4 * e4] * by, o[t][4 * e4 + 1] * by, o[t][4 * e4 + 2] * by, o[t][4 * e4 + 3] * by};
 }
 
 // Zeros to `n` rows of `bytes` (a multiple of 16) each.
