@@ -29,7 +29,8 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
     constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
-    const int head = head_of((int)(blockIdx.x % (unsigned)a.heads), a.heads), slot = a.slots - 1 - (int)(blockIdx.x / (unsigned)a.heads);
+    int head, slot;
+    place_of<CAUSAL>(a.heads, a.slots, head, slot);
     Rows r;
     if (!find_rows<Q>(a, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;

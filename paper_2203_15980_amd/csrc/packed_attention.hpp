@@ -48,26 +48,43 @@ inline int slots_of(int M, int seqs, int Q) { return M / Q + seqs + 2; }
 template <int Q>
 __device__ __forceinline__ bool find_rows(const Args &a, int slot, Rows &r) {
     const int lane = threadIdx.x & 63;
-    int lo = 0, n = a.seqs + 2;
-    while (n > 1) {
-        const int step = (n + 63) / 64, j = lo + lane * step;
-        const bool before = lane * step < n && boundary(a, j) / Q + j <= slot;
-        const int k = __builtin_popcountll(__ballot(before)) - 1;                  // lane 0's segment begins at or before the slot
-        const int at = k < 0 ? 0 : k;
+    int lo = 0, n = a.seqs + 2, step, at, mine, next;
+    do {
+        step = (n + 63) / 64;
+        const int j = lo + lane * step, last = a.seqs + 2;
+        mine = boundary(a, j < last ? j : last);
+        next = boundary(a, j + 1 < last ? j + 1 : last);                           // of use where step is 1
+        const bool before = lane * step < n && mine / Q + j <= slot;
+        at = __builtin_popcountll(__ballot(before)) - 1;                           // lane 0's segment begins at or before the slot
+        at = at < 0 ? 0 : at;
         lo += at * step;
         n = n - at * step < step ? n - at * step : step;
-    }
+    } while (step > 1);
     lo = __builtin_amdgcn_readfirstlane(lo);
-    const int b = __builtin_amdgcn_readfirstlane(boundary(a, lo)), e = __builtin_amdgcn_readfirstlane(boundary(a, lo + 1));
-    r.start = b;
-    r.len = e - b;
-    r.tile = slot - (b / Q + lo);
+    at = __builtin_amdgcn_readfirstlane(at);
+    r.start = __builtin_amdgcn_readlane(mine, at);
+    r.len = __builtin_amdgcn_readlane(next, at) - r.start;
+    r.tile = slot - (r.start / Q + lo);
     r.alone = lo == 0 || lo == a.seqs + 1;
     return r.tile >= 0 && r.tile * (long long)Q < r.len;
 }
 
 // Consecutive workgroups go to the 8 XCDs in turn, each with an L2 of its own: numbered like this, an XCD's heads are neighbours, which share keys and values.
 __device__ __forceinline__ int head_of(int i, int heads) { return heads % 8 ? i : (i & 7) * (heads >> 3) + (i >> 3); }
+// A workgroup's head and slot, of `units` heads.  The last slots first: causal, the last tiles of a sequence have the most keys.  Not causal, an XCD takes a run of one
+// head's slots after the other's.
+template <bool CAUSAL>
+__device__ __forceinline__ void place_of(int units, int slots, int &unit, int &slot) {
+    const unsigned i = blockIdx.x;
+    if (CAUSAL) {
+        unit = head_of((int)(i % (unsigned)units), units);
+        slot = slots - 1 - (int)(i / (unsigned)units);
+    } else {
+        const unsigned per = gridDim.x >> 3, rem = gridDim.x & 7u, xcd = i & 7u, k = xcd * per + (xcd < rem ? xcd : rem) + (i >> 3);
+        unit = (int)(k / (unsigned)slots);
+        slot = slots - 1 - (int)(k % (unsigned)slots);
+    }
+}
 
 // A tile of rows of D bf16 channels in LDS, without padding: piece p (16 bytes) of row r lies at piece p ^ twist(r) of its row, so that both ways of
 // reading it below meet each bank as seldom as can be: 16 lanes that read one piece of 16 rows, and 32 that read 64 bytes of four rows.

@@ -26,7 +26,8 @@ __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
     constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
-    const int head = (int)(blockIdx.x % (unsigned)a.heads), slot = a.slots - 1 - (int)(blockIdx.x / (unsigned)a.heads);
+    int head, slot;
+    place_of<CAUSAL>(a.heads, a.slots, head, slot);
     Rows r;
     if (!find_rows<Q>(a, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
@@ -135,8 +136,10 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) float stats[2][2][Q];       // of a block's queries: log-sum-exp (log2), delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
-    // first keys first: causal, they have the most queries
-    const int units = a.kv * a.splits, unit = (int)(blockIdx.x % (unsigned)units), slot = (int)(blockIdx.x / (unsigned)units), kh = unit / a.splits, split = unit % a.splits;
+    int unit, slot;
+    place_of<CAUSAL>(a.kv * a.splits, a.slots, unit, slot);
+    const int kh = unit / a.splits, split = unit % a.splits;
+    if (CAUSAL) slot = a.slots - 1 - slot;               // the first keys have the most queries
     Rows r;
     if (!find_rows<K>(a, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
