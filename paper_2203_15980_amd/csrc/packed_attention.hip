@@ -17,20 +17,22 @@
 namespace delta {
 namespace pat {
 
-constexpr int kBlock = 64;                               // keys to a block
 // The running maximum is raised (and what has been summed scaled) only where a lane's grows by more than this many powers of two: until then weights are up to 2^kLate,
 // which neither fp32 nor bf16 minds, and the quotient is the same.
 constexpr float kLate = 8.f;
 
-template <int D> constexpr int kBuffer = 2 * kTile<D>;                             // K and V of a block
+template <int D, int G> constexpr int kBuffer = 2 * kTile<D, kKeys<D, G>>;         // K and V of a block
 
-template <int D, int W, bool CAUSAL>
-__global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
-    constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
+// W wavefronts of 32 queries each, G times: group g takes the blocks g, g + G, .. of keys, and the groups' sums meet in LDS.
+template <int D, int W, int G, bool CAUSAL>
+__global__ __launch_bounds__(W * G * 64, 2) void forward_kernel(Args a) {
+    constexpr int Q = W * 32, KS = D / 16, DB = D / 32, kBlock = kKeys<D, G>, T = kBlock / 32;
     extern __shared__ __align__(16) unsigned char smem[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
+    __shared__ float meet[G > 1 ? (G - 1) * W : 1][2][64];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) % W, group = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / W;
     int head, slot;
-    place_of<CAUSAL>(a.heads, a.slots, head, slot);
+    place_of<CAUSAL>(blockIdx.x, gridDim.x, a.heads, a.slots, head, slot);
     Rows r;
     if (!find_rows<Q>(a, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
@@ -59,48 +61,50 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
     for (int t = 0; t < DB; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
-    float m_run = -__builtin_inff(), l_run = 0.f;        // l_run: this half-wave's share of the sum
+    float m_run = -3.402823466e38f, l_run = 0.f;         // finite: a lane's first blocks may hold no key of its own; l_run: this half-wave's share of the sum
     const int keys = CAUSAL && q0 + Q < r.len ? q0 + Q : r.len, blocks = (keys + kBlock - 1) / kBlock;
     const int limit = CAUSAL && q + 1 < r.len ? q + 1 : r.len;                     // the lane's keys
-    const Loader<D, W> loader(wave);
-    const uint32_t lds = lds_of(smem);
-    auto load = [&](int b) {
-        const uint32_t at = lds + (uint32_t)(b & 1) * kBuffer<D>;
+    const Loader<D, W, kBlock> loader(wave);
+    const uint32_t lds = lds_of(smem) + (uint32_t)group * 2 * kBuffer<D, G>;
+    auto load = [&](int i) {
+        const int b = i * G + group;
+        if (b >= blocks) return;
+        const uint32_t at = lds + (uint32_t)(i & 1) * kBuffer<D, G>;
         const size_t from = (size_t)b * kBlock * pitch;
         loader.load(kb + from, (uint32_t)pitch, r.len - b * kBlock, at);
-        loader.load(vb + from, (uint32_t)pitch, r.len - b * kBlock, at + kTile<D>);
+        loader.load(vb + from, (uint32_t)pitch, r.len - b * kBlock, at + kTile<D, kBlock>);
     };
     load(0);
-    for (int b = 0; b < blocks; ++b) {
+    for (int i = 0; i * G < blocks; ++i) {
         arrived();
-        __syncthreads();                                 // block b is there; block b - 1 is done with
-        if (b + 1 < blocks) load(b + 1);
-        const unsigned char *ks = smem + (b & 1) * kBuffer<D>, *vs = ks + kTile<D>;
-        const int k0 = b * kBlock;
-        if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
-            f32x16 s[2];
+        __syncthreads();                                 // the block is there; the one before is done with
+        load(i + 1);
+        const unsigned char *ks = smem + (group * 2 + (i & 1)) * kBuffer<D, G>, *vs = ks + kTile<D, kBlock>;
+        const int k0 = (i * G + group) * kBlock;
+        if (k0 < keys && w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
+            f32x16 s[T];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < T; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) s[t] = mfma(rows_of<D>(ks, 32 * t, k), qf[k], s[t]);
+                for (int t = 0; t < T; ++t) s[t] = mfma(rows_of<D>(ks, 32 * t, k), qf[k], s[t]);
             if (__builtin_expect(k0 + kBlock > (CAUSAL ? (w0 + 1 < r.len ? w0 + 1 : r.len) : r.len), 0)) {
                 const int lim = limit - k0 - 4 * half;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < T; ++t)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[t][e] = 32 * t + row_of(e) < lim ? s[t][e] : -__builtin_inff();
                 asm volatile("" ::: "memory");           // keeps the masked path a separate block
             }
             float mx = -__builtin_inff();
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < T; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[t][e]);
-            const float m_new = fmaxf(m_run, halves_max(mx) * a.scale_log2e);      // finite: key 0 is every query's
+            const float m_new = fmaxf(m_run, halves_max(mx) * a.scale_log2e);
             if (__any(m_new > m_run + kLate)) {
                 const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);         // 0 on the first block
                 m_run = m_new;
@@ -111,7 +115,7 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
                     for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
             }
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < T; ++t) {
                 float sum = 0.f;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -129,18 +133,57 @@ __global__ __launch_bounds__(W * 64, 2) void forward_kernel(Args a) {
         }
     }
     l_run = rows::halves(l_run);
+    if constexpr (G > 1) {
+        __syncthreads();                                 // the last blocks are done with
+        float *sums = reinterpret_cast<float *>(smem);
+        if (group) {
+            hand_over(sums, (group - 1) * W + wave, o);
+            meet[(group - 1) * W + wave][0][lane] = m_run;
+            meet[(group - 1) * W + wave][1][lane] = l_run;
+        }
+        __syncthreads();
+        if (group) return;
+        float m = m_run;
+#pragma unroll
+        for (int g = 0; g < G - 1; ++g) m = fmaxf(m, meet[g * W + wave][0][lane]);
+        const float mine = __builtin_amdgcn_exp2f(m_run - m);
+        l_run *= mine;
+        m_run = m;
+#pragma unroll
+        for (int t = 0; t < DB; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] *= mine;
+#pragma unroll
+        for (int g = 0; g < G - 1; ++g) {
+            const float other = __builtin_amdgcn_exp2f(meet[g * W + wave][0][lane] - m);
+            l_run += meet[g * W + wave][1][lane] * other;
+            take_over(sums, g * W + wave, o, other);
+        }
+    }
     if (!there) return;
     store_column<DB>(yb + (size_t)q * out_pitch, o, 1.0f / l_run);
     if (lse && !half) lse[q] = (m_run + __builtin_amdgcn_logf(l_run)) * 0.6931471805599453f;
 }
 
-template <int D, int W, bool CAUSAL>
+template <int D, int W, int G, bool CAUSAL>
 static hipError_t forward(Args a, hipStream_t stream) {
-    constexpr int kLds = 2 * kBuffer<D>;
-    static_assert(kLds <= 64 * 1024, "what a launch may ask for without more ado");
+    constexpr int kLds = G * 2 * kBuffer<D, G>;
+    static_assert((G - 1) * W * D / 32 * 16 * 64 * 4 <= kLds, "the sums fit where the blocks were");
+    if (kLds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&forward_kernel<D, W, G, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (e != hipSuccess) return e;
+    }
     a.slots = slots_of(a.M, a.seqs, W * 32);
-    forward_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * 64), kLds, stream>>>(a);
+    forward_kernel<D, W, G, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * G * 64), kLds, stream>>>(a);
     return hipGetLastError();
+}
+template <int D, bool CAUSAL>
+static hipError_t forward(const Args &a, hipStream_t stream) {
+    switch (groups_of(a.M, a.seqs, a.heads, D)) {
+    case 4: return forward<D, 1, 4, CAUSAL>(a, stream);
+    case 2: return forward<D, 2, 2, CAUSAL>(a, stream);
+    default: return forward<D, 4, 1, CAUSAL>(a, stream);
+    }
 }
 
 }  // namespace pat
@@ -154,8 +197,8 @@ const char *packed_attention_check(long long M, long long seqs, int Cin, int Cou
     if (Cin > 1 << 24) return "attention takes rows of at most 16777216 channels";     // 64 of them lie within 32 bits
     if (M <= 0 || M > 0x7FFFFF00LL) return "attention takes 1 to 2147483392 rows";
     if (seqs < 1 || seqs > 0x3FFFFFFFLL) return "offsets must hold one int64 value more than there are sequences";
-    // threads of a launch: 128 queries or keys to 256 threads, and a workgroup to each sequence and each end
-    if ((M / 128 + seqs + 2) * heads * 256 > 0x7FFFFFFFLL) return "too many rows, sequences and heads in one launch";
+    // threads of a launch: 32 queries or keys to 256 threads at least, and a workgroup to each sequence and each end
+    if ((M / 32 + seqs + 2) * heads * 256 > 0x7FFFFFFFLL) return "too many rows, sequences and heads in one launch";
     return nullptr;
 }
 
@@ -172,8 +215,8 @@ hipError_t launch_packed_attention(const void *x, const void *off, void *y, floa
                                    int causal, int bf16, hipStream_t stream) {
     if (!x || !off || !y || packed_attention_check(M, seqs, Cin, Cout, heads, kv, bf16)) return hipErrorInvalidValue;
     const pat::Args a = packed_attention_args(x, off, y, lse, M, seqs, Cout, heads, kv);
-    if (Cout / heads == 64) return causal ? pat::forward<64, 4, true>(a, stream) : pat::forward<64, 4, false>(a, stream);
-    return causal ? pat::forward<128, 4, true>(a, stream) : pat::forward<128, 4, false>(a, stream);
+    if (Cout / heads == 64) return causal ? pat::forward<64, true>(a, stream) : pat::forward<64, false>(a, stream);
+    return causal ? pat::forward<128, true>(a, stream) : pat::forward<128, false>(a, stream);
 }
 
 }  // namespace delta

@@ -29,6 +29,26 @@ struct Args {
     float scale, scale_log2e;                            // 1 / sqrt(D), times log2 e
 };
 
+// Keys to a block of a group's: four groups' blocks of 128 channels fit the LDS as half ones only.
+template <int D, int G> constexpr int kKeys = D == 128 && G == 4 ? 32 : 64;
+
+// Groups of wavefronts that share a tile's work: a workgroup is 4 wavefronts, each with 32 rows, and with 2 or 4 groups the tile is 64 or 32 rows and a group takes every
+// second or fourth block of what the rows meet.  Four groups until the chip has a workgroup to each CU (long sequences: two), two until it has about
+// four (heads of 128, whose blocks leave room for one on a CU: two).  us with 1, 2 and 4 groups, forward, then gradients, causal:
+//   tokens x heads (key heads) of channels   forward            gradients
+//   200 x 12 (12) of 64                      6.3, 5.7, 5.2      19.1, 15.7, 13.6
+//   512 x 12 (12) of 64                      9.7, 7.6, 6.4      29.8, 21.5, 16.8
+//   4096 x 4 (1) of 64                       50, 34, 28         183, 118, 84
+//   2048 x 32 (4) of 64                      32, 32, 65         119, 98, 195
+//   1024 x 8 (2) of 128                      24, 16, 14         90, 61, 46
+//   1024 x 32 (8) of 128                     25, 23, 37         111, 88, 120
+//   2048 x 32 (8) of 128                     51, 66, 107        217, 268, 342
+inline int groups_of(long long M, long long seqs, int units, int D) {
+    const long long tiles = (M + 31) / 32 * units;
+    if (tiles <= 256 || (tiles <= 512 && M >= 1024 * seqs)) return 4;
+    return tiles <= (D == 64 ? 2048 : 1024) ? 2 : 1;
+}
+
 // Rows of a workgroup: `tile` of the segment [start, start + len).  Segments: the rows before the first sequence, the sequences, the rows behind the last
 // (the first and the last belong to no sequence: `alone`).  Boundaries are held in [0, M], so that no offset leads out of the tensors.
 //
@@ -74,13 +94,12 @@ __device__ __forceinline__ int head_of(int i, int heads) { return heads % 8 ? i 
 // A workgroup's head and slot, of `units` heads.  The last slots first: causal, the last tiles of a sequence have the most keys.  Not causal, an XCD takes a run of one
 // head's slots after the other's.
 template <bool CAUSAL>
-__device__ __forceinline__ void place_of(int units, int slots, int &unit, int &slot) {
-    const unsigned i = blockIdx.x;
+__device__ __forceinline__ void place_of(unsigned i, unsigned n, int units, int slots, int &unit, int &slot) {       // workgroup i of n
     if (CAUSAL) {
         unit = head_of((int)(i % (unsigned)units), units);
         slot = slots - 1 - (int)(i / (unsigned)units);
     } else {
-        const unsigned per = gridDim.x >> 3, rem = gridDim.x & 7u, xcd = i & 7u, k = xcd * per + (xcd < rem ? xcd : rem) + (i >> 3);
+        const unsigned per = n >> 3, rem = n & 7u, xcd = i & 7u, k = xcd * per + (xcd < rem ? xcd : rem) + (i >> 3);
         unit = (int)(k / (unsigned)slots);
         slot = slots - 1 - (int)(k % (unsigned)slots);
     }
@@ -99,19 +118,17 @@ __device__ __forceinline__ constexpr int twist(int r) {
 template <int D, int W, int ROWS = 64>
 struct Loader {
     static constexpr int kRows = 64 * 16 / (D * 2), kTurns = ROWS / (kRows * W);   // rows of a wavefront's load; loads to a tile
-    static_assert(kTurns * kRows * W == ROWS && kRows * W % 16 == 0, "the twist of a lane's row is the same in each turn");
+    static_assert(kTurns * kRows * W == ROWS, "whole loads");
     int row, lds;
-    uint32_t piece;                                      // byte of the row
     __device__ __forceinline__ Loader(int wave) {
-        const int lane = threadIdx.x & 63;
-        row = wave * kRows + lane / (D / 8);
-        piece = (uint32_t)((lane % (D / 8)) ^ twist<D>(row)) * 16;
+        row = wave * kRows + (int)(threadIdx.x & 63) / (D / 8);
         lds = wave * kRows * D * 2;
     }
     __device__ __forceinline__ void load(const unsigned char *base, uint32_t pitch, int rows, uint32_t tile) const {
-#pragma unroll
+#pragma unroll kTurns > 4 ? 2 : kTurns
         for (int t = 0; t < kTurns; ++t) {
             const int r = row + t * kRows * W;
+            const uint32_t piece = (uint32_t)(((int)(threadIdx.x & 63) % (D / 8)) ^ twist<D>(r)) * 16;
             load_lds_b128(base, (uint32_t)(r < rows ? r : rows - 1) * pitch + piece, tile + (uint32_t)(lds + t * kRows * W * D * 2));
         }
     }
@@ -177,6 +194,24 @@ __device__ __forceinline__ void store_column(float *out, const f32x16 (&o)[BLOCK
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4)
             *reinterpret_cast<f32x4 *>(out + 32 * t + 8 * e4 + 4 * half) = f32x4{o[t][4 * e4] * by, o[t][4 * e4 + 1] * by, o[t][4 * e4 + 2] * by, o[t][4 * e4 + 3] * by};
+}
+
+// Sums of the W wavefronts of one group on their way through LDS to those of another: register e of a lane at [wavefront][e][lane].
+template <int BLOCKS>
+__device__ __forceinline__ void hand_over(float *lds, int wave, const f32x16 (&o)[BLOCKS]) {
+    float *at = lds + wave * BLOCKS * 16 * 64 + (threadIdx.x & 63);
+#pragma unroll
+    for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) at[(t * 16 + e) * 64] = o[t][e];
+}
+template <int BLOCKS>
+__device__ __forceinline__ void take_over(const float *lds, int wave, f32x16 (&o)[BLOCKS], float by) {
+    const float *at = lds + wave * BLOCKS * 16 * 64 + (threadIdx.x & 63);
+#pragma unroll
+    for (int t = 0; t < BLOCKS; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] += at[(t * 16 + e) * 64] * by;
 }
 
 // Zeros to `n` rows of `bytes` (a multiple of 16) each.

@@ -17,17 +17,16 @@ namespace delta {
 namespace pat {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kStep = 64;                                // keys (of gq's kernel) or queries (of the other's) to a block
+template <int D, int G> constexpr int kPair = 2 * kTile<D, kKeys<D, G>>;           // K and V of a block
 
-template <int D> constexpr int kPair = 2 * kTile<D>;                               // two tiles
-
-template <int D, int W, bool CAUSAL>
-__global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
-    constexpr int Q = W * 32, KS = D / 16, DB = D / 32;
-    extern __shared__ __align__(16) unsigned char smem[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
+// W wavefronts of 32 queries each, G times: the groups take turns at the blocks of keys, and their sums meet in LDS.
+template <int D, int W, int G, bool CAUSAL>
+__device__ __forceinline__ void gq_tile(const Args &a, unsigned block, unsigned blocks_of_launch, unsigned char *smem) {
+    constexpr int Q = W * 32, KS = D / 16, DB = D / 32, kStep = kKeys<D, G>;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) % W, group = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / W;
     int head, slot;
-    place_of<CAUSAL>(a.heads, a.slots, head, slot);
+    place_of<CAUSAL>(block, blocks_of_launch, a.heads, a.slots, head, slot);
     Rows r;
     if (!find_rows<Q>(a, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
@@ -65,7 +64,7 @@ __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
     delta = rows::halves(delta);
     const size_t stat = (size_t)head * a.M + r.start + row;
     const float lse2 = a.lse[stat] * kLog2e;
-    if (there && !half) a.delta[stat] = delta;
+    if (there && !half && !group) a.delta[stat] = delta;
     f32x16 g[DB];
 #pragma unroll
     for (int t = 0; t < DB; ++t)
@@ -73,26 +72,28 @@ __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
         for (int e = 0; e < 16; ++e) g[t][e] = 0.f;
     const int keys = CAUSAL && q0 + Q < r.len ? q0 + Q : r.len, blocks = (keys + kStep - 1) / kStep;
     const int limit = CAUSAL && q + 1 < r.len ? q + 1 : r.len;
-    const Loader<D, W> loader(wave);
-    const uint32_t lds = lds_of(smem);
-    auto load = [&](int b) {
-        const uint32_t at = lds + (uint32_t)(b & 1) * kPair<D>;
+    const Loader<D, W, kStep> loader(wave);
+    const uint32_t lds = lds_of(smem) + (uint32_t)group * 2 * kPair<D, G>;
+    auto load = [&](int i) {
+        const int b = i * G + group;
+        if (b >= blocks) return;
+        const uint32_t at = lds + (uint32_t)(i & 1) * kPair<D, G>;
         const size_t from = (size_t)b * kStep * pitch;
         loader.load(kb + from, (uint32_t)pitch, r.len - b * kStep, at);
-        loader.load(vb + from, (uint32_t)pitch, r.len - b * kStep, at + kTile<D>);
+        loader.load(vb + from, (uint32_t)pitch, r.len - b * kStep, at + kTile<D, kStep>);
     };
     load(0);
-    for (int b = 0; b < blocks; ++b) {
+    for (int i = 0; i * G < blocks; ++i) {
         arrived();
-        __syncthreads();                                 // block b is there; block b - 1 is done with
-        if (b + 1 < blocks) load(b + 1);
-        const unsigned char *ks = smem + (b & 1) * kPair<D>, *vs = ks + kTile<D>;
-        const int k0 = b * kStep;
-        if (w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
+        __syncthreads();                                 // the block is there; the one before is done with
+        load(i + 1);
+        const unsigned char *ks = smem + (group * 2 + (i & 1)) * kPair<D, G>, *vs = ks + kTile<D, kStep>;
+        const int k0 = (i * G + group) * kStep;
+        if (k0 < keys && w0 < r.len && (!CAUSAL || k0 <= w0 + 31)) {
             const bool border = k0 + kStep > (CAUSAL ? (w0 + 1 < r.len ? w0 + 1 : r.len) : r.len);
             const int lim = border ? limit - k0 - 4 * half : kStep;
 #pragma unroll 1
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < kStep / 32; ++t) {
                 __builtin_amdgcn_sched_barrier(0);       // one tile after the other: both at once do not fit the registers
                 f32x16 s, dp;
 #pragma unroll
@@ -121,27 +122,39 @@ __global__ __launch_bounds__(W * 64, 2) void gq_kernel(Args a) {
             }
         }
     }
+    if constexpr (G > 1) {
+        __syncthreads();                                 // the last blocks are done with
+        float *sums = reinterpret_cast<float *>(smem);
+        if (group) hand_over(sums, (group - 1) * W + wave, g);
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int other = 0; other < G - 1; ++other) take_over(sums, other * W + wave, g, 1.0f);
+    }
     if (there) store_column<DB>(gxb + (size_t)q * pitch, g, a.scale);
 }
 
 // Heads of 128: a lane's sums of gk and gv, its key and its value would be 192 registers of the 256 that two wavefronts to a SIMD leave: the values stay in LDS, and
 // with them (32 KB) and another workgroup's there is room for blocks of 32 queries.
 template <int D> constexpr int kQueries = D == 128 ? 32 : 64;
-template <int D, int W> constexpr int kKvLds = 4 * kTile<D, kQueries<D>> + (D == 128 ? kTile<D, W * 32> : 0);
+template <int D, int W, int G> constexpr int kKvLds = G * 4 * kTile<D, kQueries<D>> + (D == 128 ? kTile<D, W * 32> : 0);
 
-template <int D, int W, bool CAUSAL>
-__global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
+// OWN: with delta made here, for all queries that the keys may meet, instead of read: both kernels are one launch then.
+constexpr int kOwn = 2048;
+template <int D, int W, int G, bool CAUSAL, bool OWN>
+__device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsigned workgroups, unsigned char *smem) {
     constexpr int K = W * 32, KS = D / 16, DB = D / 32, Q = kQueries<D>;
     constexpr bool kValuesInLds = D == 128;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ __align__(16) float stats[2][2][Q];       // of a block's queries: log-sum-exp (log2), delta
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l32 = lane & 31, half = lane >> 5;
+    __shared__ __align__(16) float own[OWN ? kOwn : 4];  // [head of the share][query, to whole blocks]
+    __shared__ __align__(16) float stats[G][2][2][Q];    // of a block's queries: log-sum-exp (log2), delta
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5, thread = (int)threadIdx.x % (W * 64);
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) % W, group = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / W;
     int unit, slot;
-    place_of<CAUSAL>(a.kv * a.splits, a.slots, unit, slot);
+    place_of<CAUSAL>(workgroup, workgroups, a.kv * a.splits, a.slots, unit, slot);
     const int kh = unit / a.splits, split = unit % a.splits;
-    if (CAUSAL) slot = a.slots - 1 - slot;               // the first keys have the most queries
     Rows r;
     if (!find_rows<K>(a, slot, r)) return;
+    if (CAUSAL) r.tile = (r.len - 1) / K - r.tile;       // a sequence's first keys have the most queries
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
     const int first = r.tile * K, share = a.heads / a.kv / a.splits;                // query heads of this workgroup
     unsigned char *gkb = a.gx + (size_t)r.start * pitch + (size_t)(a.heads + kh) * D * 2, *gvb = gkb + (size_t)a.kv * D * 2;
@@ -161,8 +174,8 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
     const unsigned char *xb = a.x + (size_t)r.start * pitch;
     const int w0 = first + 32 * wave, key = w0 + l32;
     const bool there = key < r.len;
-    const uint32_t lds = lds_of(smem);
-    const unsigned char *values = smem + 4 * kTile<D, Q>;
+    const uint32_t lds = lds_of(smem) + (uint32_t)group * 4 * kTile<D, Q>;
+    const unsigned char *tiles = smem + group * 4 * kTile<D, Q>, *values = smem + G * 4 * kTile<D, Q>;
     bf16x8 kf[KS], vf[kValuesInLds ? 1 : KS];
     {
         const unsigned char *p = xb + (size_t)(there ? key : r.len - 1) * pitch + (size_t)(a.heads + kh) * D * 2 + half * 16;
@@ -173,7 +186,7 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
         }
     }
     if constexpr (kValuesInLds)
-        Loader<D, W, K>(wave).load(xb + (size_t)first * pitch + (size_t)(a.heads + a.kv + kh) * D * 2, (uint32_t)pitch, r.len - first, lds + 4 * kTile<D, Q>);
+        Loader<D, W * G, K>(group * W + wave).load(xb + (size_t)first * pitch + (size_t)(a.heads + a.kv + kh) * D * 2, (uint32_t)pitch, r.len - first, lds_of(values));
     f32x16 gk[DB], gv[DB];
 #pragma unroll
     for (int t = 0; t < DB; ++t)
@@ -186,24 +199,55 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
         const uint32_t to = lds + (uint32_t)buffer * 2 * kTile<D, Q>;
         loader.load(xb + (size_t)at * pitch + (size_t)head * D * 2, (uint32_t)pitch, r.len - at, to);
         loader.load(a.gy + ((size_t)r.start + at) * out_pitch + (size_t)head * D * 2, (uint32_t)out_pitch, r.len - at, to + kTile<D, Q>);
-        const int q = at + ((int)threadIdx.x & (Q - 1));
-        if (threadIdx.x < Q) st = q < r.len ? a.lse[(size_t)head * a.M + r.start + q] * kLog2e : __builtin_inff();      // p = 0 behind the last query
-        else if (threadIdx.x < 2 * Q) st = q < r.len ? a.delta[(size_t)head * a.M + r.start + q] : 0.f;
+        const int q = at + (thread & (Q - 1));
+        if (thread < Q) st = q < r.len ? a.lse[(size_t)head * a.M + r.start + q] * kLog2e : __builtin_inff();      // p = 0 behind the last query
+        else if (!OWN && thread < 2 * Q) st = q < r.len ? a.delta[(size_t)head * a.M + r.start + q] : 0.f;
     };
-    // Each head's queries from the last block on backwards: causal, workgroups on an XCD begin at the same block and find it in its L2.
+    // Each head's queries from the last block on backwards: causal, workgroups on an XCD begin at the same block and find it in its L2.  The groups take turns at the
+    // blocks of all heads in one row.
     const int end = (kh * a.splits + split + 1) * share;
     int head = end - share, block = per - 1, buffer = 0;
-    load(head, (begin + block) * Q, 0);
-    for (;;) {
-        if (threadIdx.x < 2 * Q) stats[buffer][threadIdx.x / Q][threadIdx.x & (Q - 1)] = st;
+    auto go_on = [&](int n) {
+        for (block -= n; block < 0; block += per) ++head;
+    };
+    go_on(group);
+    if (head < end) load(head, (begin + block) * Q, 0);
+    const int span = (begin + per) * Q;
+    if constexpr (OWN) {
+        const int part = (int)threadIdx.x & 3;
+        for (int i = (int)threadIdx.x >> 2; i < share * span; i += W * G * 16) {
+            const int h = i / span, q = i - h * span;
+            float sum = 0.f;
+            if (q < r.len) {
+                const size_t at = ((size_t)r.start + q) * out_pitch + (size_t)(end - share + h) * D * 2 + part * (D / 2);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    rows::Eight<rows::bf16> g, y;
+                    g.load(a.gy + at + c * 16);
+                    y.load(a.y + at + c * 16);
+                    float u[8], v[8];
+                    g.to(u);
+                    y.to(v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += u[e] * v[e];
+                }
+            }
+            sum += rows::dpp<0xB1>(sum);
+            sum += rows::dpp<0x4E>(sum);
+            if (!part) own[i] = sum;
+        }
+    }
+    for (int i = 0; i * G < per * share; ++i) {
+        if (thread < 2 * Q) stats[group][buffer][thread / Q][thread & (Q - 1)] = st;
         arrived();
         __syncthreads();                                 // the block is there; the one before is done with
         const int at = (begin + block) * Q;
-        if (block-- == 0) { block = per - 1; ++head; }
-        const bool more = head < end;
-        if (more) load(head, (begin + block) * Q, buffer ^ 1);
-        const unsigned char *qs = smem + buffer * 2 * kTile<D, Q>, *gs = qs + kTile<D, Q>;
-        if (w0 < r.len && (!CAUSAL || at + Q - 1 >= w0)) {
+        const bool some = head < end;
+        const float *deltas = OWN ? own + (some ? head - (end - share) : 0) * span + at : stats[group][buffer][1];
+        go_on(G);
+        if (head < end) load(head, (begin + block) * Q, buffer ^ 1);
+        const unsigned char *qs = tiles + buffer * 2 * kTile<D, Q>, *gs = qs + kTile<D, Q>;
+        if (some && w0 < r.len && (!CAUSAL || at + Q - 1 >= w0)) {
 #pragma unroll
             for (int t = 0; t < Q / 32; ++t) {
                 __builtin_amdgcn_sched_barrier(0);       // one tile after the other
@@ -218,8 +262,8 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
                 }
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
-                    const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][32 * t + 8 * e4 + 4 * half]);
-                    const f32x4 dl = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][32 * t + 8 * e4 + 4 * half]);
+                    const f32x4 l = *reinterpret_cast<const f32x4 *>(&stats[group][buffer][0][32 * t + 8 * e4 + 4 * half]);
+                    const f32x4 dl = *reinterpret_cast<const f32x4 *>(deltas + 32 * t + 8 * e4 + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * e4 + e], a.scale_log2e, -l[e]));
@@ -247,8 +291,22 @@ __global__ __launch_bounds__(W * 64, 2) void gkv_kernel(Args a) {
                 }
             }
         }
-        if (!more) break;
         buffer ^= 1;
+    }
+    if constexpr (G > 1) {
+        float *sums = reinterpret_cast<float *>(smem);
+        __syncthreads();                                 // the last blocks are done with
+        if (group) hand_over(sums, (group - 1) * W + wave, gk);
+        __syncthreads();
+        if (!group)
+#pragma unroll
+            for (int other = 0; other < G - 1; ++other) take_over(sums, other * W + wave, gk, 1.0f);
+        __syncthreads();
+        if (group) hand_over(sums, (group - 1) * W + wave, gv);
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int other = 0; other < G - 1; ++other) take_over(sums, other * W + wave, gv, 1.0f);
     }
     if (!there) return;
     if (a.part) {
@@ -278,20 +336,75 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, uint32_t n, uint32_t 
     }
 }
 
-template <int D, int W, bool CAUSAL>
-static hipError_t backward(Args a, hipStream_t stream) {
-    constexpr int kLds = 2 * kPair<D>, kLdsKv = kKvLds<D, W>;
-    static_assert(kLds <= 64 * 1024 && kLdsKv <= 64 * 1024, "what a launch may ask for without more ado");
-    a.slots = slots_of(a.M, a.seqs, W * 32);
-    gq_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * 64), kLds, stream>>>(a);
-    hipError_t e = hipGetLastError();
+template <int D, int W, int G, bool CAUSAL>
+__global__ __launch_bounds__(W * G * 64, 2) void gq_kernel(Args a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    gq_tile<D, W, G, CAUSAL>(a, blockIdx.x, gridDim.x, smem);
+}
+template <int D, int W, int G, bool CAUSAL>
+__global__ __launch_bounds__(W * G * 64, 2) void gkv_kernel(Args a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    gkv_tile<D, W, G, CAUSAL, false>(a, blockIdx.x, gridDim.x, smem);
+}
+template <int D, int W, int G, bool CAUSAL>
+__global__ __launch_bounds__(W * G * 64, 2) void both_kernel(Args a, unsigned queries) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    if (blockIdx.x < queries) gq_tile<D, W, G, CAUSAL>(a, blockIdx.x, queries, smem);
+    else gkv_tile<D, W, G, CAUSAL, true>(a, blockIdx.x - queries, gridDim.x - queries, smem);
+}
+
+template <typename KERNEL>
+static hipError_t allow(KERNEL kernel, int lds) {
+    return lds > 64 * 1024 ? hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) : hipSuccess;
+}
+template <int D, int W, int G, bool CAUSAL>
+static hipError_t launch_gq(Args a, hipStream_t stream) {
+    constexpr int kLds = G * 2 * kPair<D, G>;
+    static_assert((G - 1) * W * D / 32 * 16 * 64 * 4 <= kLds, "the sums fit where the blocks were");
+    const hipError_t e = allow(&gq_kernel<D, W, G, CAUSAL>, kLds);
     if (e != hipSuccess) return e;
-    gkv_kernel<D, W, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)(a.kv * a.splits)), dim3(W * 64), kLdsKv, stream>>>(a);
-    e = hipGetLastError();
+    a.slots = slots_of(a.M, a.seqs, W * 32);
+    gq_kernel<D, W, G, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)a.heads), dim3(W * G * 64), kLds, stream>>>(a);
+    return hipGetLastError();
+}
+template <int D, int W, int G, bool CAUSAL>
+static hipError_t launch_gkv(Args a, hipStream_t stream) {
+    constexpr int kLds = kKvLds<D, W, G>;
+    static_assert((G - 1) * W * D / 32 * 16 * 64 * 4 <= kLds, "the sums fit where the blocks were");
+    const hipError_t e = allow(&gkv_kernel<D, W, G, CAUSAL>, kLds);
+    if (e != hipSuccess) return e;
+    a.slots = slots_of(a.M, a.seqs, W * 32);
+    gkv_kernel<D, W, G, CAUSAL><<<dim3((unsigned)a.slots * (unsigned)(a.kv * a.splits)), dim3(W * G * 64), kLds, stream>>>(a);
+    return hipGetLastError();
+}
+template <int D, bool CAUSAL>
+static hipError_t launch_both(Args a, hipStream_t stream) {
+    constexpr int W = 1, G = 4, kLdsQ = G * 2 * kPair<D, G>, kLds = kLdsQ > kKvLds<D, W, G> ? kLdsQ : kKvLds<D, W, G>;
+    const hipError_t e = allow(&both_kernel<D, W, G, CAUSAL>, kLds);
+    if (e != hipSuccess) return e;
+    a.slots = slots_of(a.M, a.seqs, W * 32);
+    const unsigned queries = (unsigned)a.slots * (unsigned)a.heads;
+    both_kernel<D, W, G, CAUSAL><<<dim3(queries + (unsigned)a.slots * (unsigned)(a.kv * a.splits)), dim3(W * G * 64), kLds, stream>>>(a, queries);
+    return hipGetLastError();
+}
+
+template <int D, bool CAUSAL>
+static hipError_t backward(const Args &a, hipStream_t stream) {
+    hipError_t e;
+    const int gq = groups_of(a.M, a.seqs, a.heads, D), gkv = groups_of(a.M, a.seqs, a.kv * a.splits, D);
+    // one launch for both while it has at most two workgroups to a CU (1024 tokens, 12 heads of 64: 38.5 us, two launches 31)
+    const long long tiles = (long long)(a.M + 31) / 32 * (a.heads + a.kv * a.splits);
+    if (gq == 4 && gkv == 4 && tiles <= 512 && (long long)(a.heads / a.kv / a.splits) * (a.M + 64) <= kOwn) {
+        e = launch_both<D, CAUSAL>(a, stream);
+    } else {
+        e = gq == 4 ? launch_gq<D, 1, 4, CAUSAL>(a, stream) : gq == 2 ? launch_gq<D, 2, 2, CAUSAL>(a, stream) : launch_gq<D, 4, 1, CAUSAL>(a, stream);
+        if (e != hipSuccess) return e;
+        e = gkv == 4 ? launch_gkv<D, 1, 4, CAUSAL>(a, stream) : gkv == 2 ? launch_gkv<D, 2, 2, CAUSAL>(a, stream) : launch_gkv<D, 4, 1, CAUSAL>(a, stream);
+    }
     if (e != hipSuccess || a.splits == 1) return e;
     const uint32_t n = (uint32_t)(2 * a.kv * D);
-    const uint64_t groups = ((uint64_t)a.M * (n / 8) + 255) / 256;
-    join_kernel<<<dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, stream>>>(a, n, (uint32_t)(a.heads * D * 2) + n * 2, (uint32_t)(a.heads * D * 2));
+    const uint64_t pieces = ((uint64_t)a.M * (n / 8) + 255) / 256;
+    join_kernel<<<dim3((unsigned)(pieces < 4096 ? pieces : 4096)), dim3(256), 0, stream>>>(a, n, (uint32_t)(a.heads * D * 2) + n * 2, (uint32_t)(a.heads * D * 2));
     return hipGetLastError();
 }
 
@@ -326,8 +439,8 @@ hipError_t launch_packed_attention_bwd(const void *x, const void *off, const voi
     a.part = a.splits > 1 ? reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + delta_bytes(M, heads)) : nullptr;
     a.scale = 1.0f / sqrtf((float)(Cout / heads));
     a.scale_log2e = a.scale * pat::kLog2e;
-    if (Cout / heads == 64) return causal ? pat::backward<64, 4, true>(a, stream) : pat::backward<64, 4, false>(a, stream);
-    return causal ? pat::backward<128, 4, true>(a, stream) : pat::backward<128, 4, false>(a, stream);
+    if (Cout / heads == 64) return causal ? pat::backward<64, true>(a, stream) : pat::backward<64, false>(a, stream);
+    return causal ? pat::backward<128, true>(a, stream) : pat::backward<128, false>(a, stream);
 }
 
 }  // namespace delta
