@@ -151,29 +151,42 @@ __global__ __launch_bounds__(1024) void forward_wide_kernel(Args a) {
     forward_rows<T, FMT, 1, 1>(a, blockIdx.x, gridDim.x, threadIdx.x, GroupSum(), slots);
 }
 
-// ---- backward: workers are persistent over rows and keep their sums of dgamma
-template <typename T, int R, int STRIDE, typename SUM>
+// ---- backward: workers are persistent over rows and keep their sums of dgamma; DEEP rows are on their way while one is worked on
+template <typename T, bool ADD, int R, int STRIDE, int DEEP, typename SUM>
 __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint32_t step, uint32_t ck0, const SUM &sum, float *slots, float (&dg)[R][8]) {
     constexpr uint32_t kEs = (uint32_t)sizeof(T);
+    rows::Eight<T> sr[DEEP][R], gr[DEEP][R];
+    auto fetch = [&](uint32_t m, int d) {
+        const uint64_t at = (uint64_t)m * a.C * kEs;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint32_t ck = ck0 + STRIDE * r;
+            if (ck * 8 >= a.C) continue;
+            sr[d][r].load(a.x + at + ck * 8 * kEs);
+            gr[d][r].load(a.gy + at + ck * 8 * kEs);
+        }
+    };
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int e = 0; e < 8; ++e) dg[r][e] = 0.f;
-    for (; row < a.rows; row += step) {
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) { sr[d][r].zero(); gr[d][r].zero(); }
+        if ((uint64_t)row + (uint64_t)d * step < a.rows) fetch(row + d * step, d);
+    }
+    auto work = [&](uint32_t row, int d) {
         const uint64_t at = (uint64_t)row * a.C * kEs;
         float s[R][8], g[R][8];
+        rows::Eight<T> w[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const uint32_t ck = ck0 + STRIDE * r;
-            rows::Eight<T> v, w;
-            v.zero(); w.zero();
-            if (ck * 8 < a.C) {
-                v.load(a.x + at + ck * 8 * kEs);
-                w.load(a.gy + at + ck * 8 * kEs);
-            }
-            v.to(s[r]);
-            w.to(g[r]);
+            sr[d][r].to(s[r]);
+            gr[d][r].to(g[r]);
+            if (ADD && (ck0 + STRIDE * r) * 8 < a.C) w[r].load(a.add + at + (ck0 + STRIDE * r) * 8 * kEs);
         }
+        if ((uint64_t)row + (uint64_t)DEEP * step < a.rows) fetch(row + DEEP * step, d);
         const float rstd = inverse_rms<R>(s, a, sum, slots);
         float dot = 0.f;
 #pragma unroll
@@ -191,34 +204,37 @@ __device__ __forceinline__ void backward_rows(const Args &a, uint32_t row, uint3
             }
         }
         const float m = sum(dot, slots + 16) * (1.0f / (float)a.C) * rstd;
-        if (!a.gx) continue;
+        if (!a.gx) return;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint32_t ck = ck0 + STRIDE * r;
             if (ck * 8 >= a.C) continue;
             float o[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = g[r][e] * rstd - s[r][e] * m;
-            if (a.add) {
-                rows::Eight<T> w;
+            for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(-s[r][e], m, g[r][e] * rstd);
+            if (ADD) {
                 float b[8];
-                w.load(a.add + at + ck * 8 * kEs);
-                w.to(b);
+                w[r].to(b);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] += b[e];
             }
             rows::Eight<T>::store(a.gx + at + ck * 8 * kEs, o);
         }
-    }
+    };
+#pragma unroll 1
+    for (uint64_t m = row; m < a.rows; m += (uint64_t)DEEP * step)
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d)
+            if (m + (uint64_t)d * step < a.rows) work((uint32_t)(m + (uint64_t)d * step), d);
 }
 
 // A row to a wavefront; the wavefronts' sums meet in LDS, in their order.
-template <typename T, int R>
+template <typename T, bool ADD, int R>
 __global__ __launch_bounds__(512) void backward_kernel(Args a) {
     extern __shared__ __align__(16) float shared[];
     const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     float dg[R][8];
-    backward_rows<T, R, 64>(a, blockIdx.x * 8 + wave, gridDim.x * 8, lane, WaveSum(), nullptr, dg);
+    backward_rows<T, ADD, R, 64, 1>(a, blockIdx.x * 8 + wave, gridDim.x * 8, lane, WaveSum(), nullptr, dg);
     if (!a.partial) return;
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -231,11 +247,11 @@ __global__ __launch_bounds__(512) void backward_kernel(Args a) {
         a.partial[(uint64_t)blockIdx.x * a.C + c] = s;
     }
 }
-template <typename T>
+template <typename T, bool ADD>
 __global__ __launch_bounds__(1024) void backward_wide_kernel(Args a) {
     __shared__ float slots[32];                          // two sums a row: a slot is rewritten two barriers after it was read
     float dg[1][8];
-    backward_rows<T, 1, 1>(a, blockIdx.x, gridDim.x, threadIdx.x, GroupSum(), slots, dg);
+    backward_rows<T, ADD, 1, 1, 2>(a, blockIdx.x, gridDim.x, threadIdx.x, GroupSum(), slots, dg);
     if (a.partial && threadIdx.x * 8 < a.C) store8(a.partial + (uint64_t)blockIdx.x * a.C + threadIdx.x * 8, dg[0]);
 }
 
@@ -314,16 +330,16 @@ hipError_t launch_rmsnorm(const void *x, const void *res, void *y, void *sum, vo
 
 size_t rmsnorm_bwd_workspace_bytes(long long rows, int C) { return (size_t)rms::workgroups(rows, C) * C * sizeof(float); }
 
-template <typename T>
+template <typename T, bool ADD>
 static hipError_t rmsnorm_backward(const rms::Args &a, uint32_t grid, hipStream_t stream) {
     if (a.C > rms::kWaveChannels) {
-        rms::backward_wide_kernel<T><<<dim3(grid), dim3((a.C / 8 + 63) / 64 * 64), 0, stream>>>(a);
+        rms::backward_wide_kernel<T, ADD><<<dim3(grid), dim3((a.C / 8 + 63) / 64 * 64), 0, stream>>>(a);
         return hipGetLastError();
     }
     auto run = [&](auto kernel) { kernel<<<dim3(grid), dim3(512), 8 * a.C * sizeof(float), stream>>>(a); };
-    if (a.C <= 512) run(rms::backward_kernel<T, 1>);
-    else if (a.C <= 1024) run(rms::backward_kernel<T, 2>);
-    else run(rms::backward_kernel<T, 4>);
+    if (a.C <= 512) run(rms::backward_kernel<T, ADD, 1>);
+    else if (a.C <= 1024) run(rms::backward_kernel<T, ADD, 2>);
+    else run(rms::backward_kernel<T, ADD, 4>);
     return hipGetLastError();
 }
 
@@ -337,7 +353,8 @@ hipError_t launch_rmsnorm_bwd(const void *s, const void *gy, const void *add, vo
     a.gx = static_cast<unsigned char *>(gx); a.gamma = gamma; a.partial = gw ? static_cast<float *>(workspace) : nullptr;
     a.rows = (uint32_t)rows; a.C = (uint32_t)C; a.eps = eps;
     const uint32_t grid = rms::workgroups(rows, C);
-    const hipError_t e = bf16 ? rmsnorm_backward<rows::bf16>(a, grid, stream) : rmsnorm_backward<float>(a, grid, stream);
+    const hipError_t e = bf16 ? (add ? rmsnorm_backward<rows::bf16, true>(a, grid, stream) : rmsnorm_backward<rows::bf16, false>(a, grid, stream))
+                              : (add ? rmsnorm_backward<float, true>(a, grid, stream) : rmsnorm_backward<float, false>(a, grid, stream));
     if (e != hipSuccess || !gw) return e;
     rms::sums_kernel<<<dim3((unsigned)(C + 15) / 16), dim3(1024), 0, stream>>>(a.partial, gw, grid, (uint32_t)C);
     return hipGetLastError();
