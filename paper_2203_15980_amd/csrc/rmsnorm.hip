@@ -277,6 +277,115 @@ __global__ __launch_bounds__(1024) void sums_kernel(const float *partial, float 
     out[c] = s;
 }
 
+// Few rows: one launch for both gradients.  A workgroup owns 64 channels and needs every row's r and mean(g sh), which it makes for itself: all threads go over all values,
+// eight at a time, four threads' sums (a block of 32 channels, never of two rows) go to LDS, eight threads to a row add those; then the same eight make the row's
+// gx of the 64 channels, and the rows' terms of dgamma meet in a fixed order.
+constexpr int kFew = 128;
+constexpr uint32_t kFewValues = 16384;
+template <typename T> constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;              // pieces of a thread on their way
+template <typename T>
+__global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor per_row) {
+    constexpr uint32_t kEs = (uint32_t)sizeof(T);
+    __shared__ float sums[2][kFewValues / 32];
+    __shared__ __align__(16) float parts[16][64];
+    const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t row = threadIdx.x >> 3, ck = blockIdx.x * 8 + (threadIdx.x & 7);
+    const bool mine = row < a.rows && ck * 8 < a.C;
+    const uint64_t at = ((uint64_t)row * a.C + ck * 8) * kEs;
+    rows::Eight<T> sr, gr, ar;
+    sr.zero(); gr.zero(); ar.zero();
+    if (mine) {                                          // on their way under the first part
+        sr.load(a.x + at);
+        gr.load(a.gy + at);
+        if (a.add) ar.load(a.add + at);
+    }
+    const uint32_t pieces = a.rows * (a.C / 8);
+#pragma unroll 1
+    for (uint32_t i0 = threadIdx.x; i0 < pieces; i0 += kAtOnce<T> * 1024) {
+        rows::Eight<T> u[kAtOnce<T>], w[kAtOnce<T>];
+        float gm[kAtOnce<T>][8];
+#pragma unroll
+        for (int k = 0; k < kAtOnce<T>; ++k) {
+            const uint32_t i = i0 + k * 1024;
+            if (i >= pieces) continue;
+            u[k].load(a.x + (uint64_t)i * 8 * kEs);
+            w[k].load(a.gy + (uint64_t)i * 8 * kEs);
+            load8(a.gamma + (i - (uint32_t)divide((int)i, per_row) * (a.C / 8)) * 8, gm[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce<T>; ++k) {
+            const uint32_t i = i0 + k * 1024;
+            if (i >= pieces) continue;                   // whole fours of threads: C is a multiple of 32
+            float s[8], g[8], q = 0.f, dot = 0.f;
+            u[k].to(s);
+            w[k].to(g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                q += s[e] * s[e];
+                dot += g[e] * gm[k][e] * s[e];
+            }
+            q += rows::dpp<0xB1>(q);
+            dot += rows::dpp<0xB1>(dot);
+            q += rows::dpp<0x4E>(q);
+            dot += rows::dpp<0x4E>(dot);
+            if ((lane & 3) == 0) { sums[0][i / 4] = q; sums[1][i / 4] = dot; }
+        }
+    }
+    __syncthreads();
+    float inverse = 0.f, mean = 0.f;
+    {
+        const uint32_t n = a.C / 32;
+        float q = 0.f, dot = 0.f;
+        if (row < a.rows)
+            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) { q += sums[0][row * n + i]; dot += sums[1][row * n + i]; }
+        q += rows::dpp<0xB1>(q);
+        dot += rows::dpp<0xB1>(dot);
+        q += rows::dpp<0x4E>(q);
+        dot += rows::dpp<0x4E>(dot);
+        q += rows::dpp<0x141>(q);                        // row_half_mirror: the other quad of a lane's eight
+        dot += rows::dpp<0x141>(dot);
+        const float over = 1.0f / (float)a.C;
+        inverse = 1.0f / sqrtf(q * over + a.eps);
+        mean = dot * over * inverse;
+    }
+    float s[8], g[8], dg[8];
+    sr.to(s);
+    gr.to(g);
+    const float r = mine ? inverse : 0.f, m = mean * r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        s[e] *= r;
+        dg[e] = g[e] * s[e];
+    }
+    if (mine && a.gx) {
+        float gm[8], o[8], b[8];
+        load8(a.gamma + ck * 8, gm);
+        ar.to(b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            o[e] = __builtin_fmaf(-s[e], m, g[e] * gm[e] * r);
+            if (a.add) o[e] += b[e];
+        }
+        rows::Eight<T>::store(a.gx + at, o);
+    }
+    if (!gw) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {                        // the wavefront's eight rows
+        dg[e] += rows::dpp<0x128>(dg[e]);                // row_ror:8
+        dg[e] = rows::halves(rows::row_pairs(dg[e]));
+    }
+    if (lane < 8) store8(&parts[wave][lane * 8], dg);
+    __syncthreads();
+    const uint32_t c = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || c >= a.C) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += parts[w][threadIdx.x];
+    gw[c] = sum;
+}
+// us with gx_add, bf16: 1 x 4096 3.8, 128 x 64 4.1, two launches 6.2 whatever the size up to 77 x 768, which takes 7.0 like this: a workgroup reads everything.
+constexpr bool few_rows(uint64_t rows, uint64_t C) { return rows <= kFew && rows * C <= kFewValues && C % 32 == 0; }
+
 // Workgroups of the backward launch, a partial sum of dgamma to each.
 uint32_t workgroups(long long rows, int C) {
     const long long per = C <= kWaveChannels ? 8 : 1, most = C <= kWaveChannels ? 256 : 512;
@@ -352,6 +461,13 @@ hipError_t launch_rmsnorm_bwd(const void *s, const void *gy, const void *add, vo
     a.x = static_cast<const unsigned char *>(s); a.gy = static_cast<const unsigned char *>(gy); a.add = static_cast<const unsigned char *>(add);
     a.gx = static_cast<unsigned char *>(gx); a.gamma = gamma; a.partial = gw ? static_cast<float *>(workspace) : nullptr;
     a.rows = (uint32_t)rows; a.C = (uint32_t)C; a.eps = eps;
+    if (rms::few_rows((uint64_t)rows, (uint64_t)C)) {
+        const dim3 columns((unsigned)(C + 63) / 64);
+        const Divisor per_row = make_divisor((uint32_t)C / 8);
+        if (bf16) rms::few_kernel<rows::bf16><<<columns, dim3(1024), 0, stream>>>(a, gw, per_row);
+        else rms::few_kernel<float><<<columns, dim3(1024), 0, stream>>>(a, gw, per_row);
+        return hipGetLastError();
+    }
     const uint32_t grid = rms::workgroups(rows, C);
     const hipError_t e = bf16 ? (add ? rmsnorm_backward<rows::bf16, true>(a, grid, stream) : rmsnorm_backward<rows::bf16, false>(a, grid, stream))
                               : (add ? rmsnorm_backward<float, true>(a, grid, stream) : rmsnorm_backward<float, false>(a, grid, stream));

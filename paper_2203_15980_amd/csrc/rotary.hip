@@ -7,7 +7,8 @@
 // 2^-51 of the angle: 5e-7 at 2^31 radians), then a fraction of an eighth of a turn at most goes to fp32 and into the Taylor polynomials of sine and
 // cosine (to x^9 and x^10: what is left out is below 2e-9).  Computed once a token, by the wavefront that turns its row, and read from LDS for each head.
 //
-// Bound by memory: each value is read and written once.
+// Bound by memory: each value is read and written once.  bf16, 8192 rows of 48 heads of 128, 40 of them rotated, 32 us (201 MB, 6.2 TB/s, part of it from the L2s'
+// shared cache; 45 us, 4.5 TB/s, from HBM); fp32 84 us (403 MB, 4.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,6 +21,7 @@ namespace rot {
 using rows::f32x4;
 
 constexpr int kMostD = 256, kMostAxes = 8, kWaves = 4;
+constexpr uint32_t kAngles = 512;                        // of a wavefront's rows: D / 2 each
 
 struct Args {
     const unsigned char *x;
@@ -28,7 +30,8 @@ struct Args {
     const float *freq;                                   // [axes][D / 2]
     uint32_t rows, axes, D;
     uint32_t turned, units;                              // pieces of 16 channels of a row: of the rotated heads, all
-    Divisor per_head;                                    // by D / 16
+    uint32_t tokens;                                     // rows of a wavefront at a time
+    Divisor per_head, per_half, per_row;                 // by D / 16, by D / 2, by units
     float sign;
 };
 
@@ -43,45 +46,49 @@ __device__ __forceinline__ void turn_of(double t, float &c, float &s) {
     s = n == 0 ? sn : n == 1 ? cs : n == 2 ? -sn : -cs;
 }
 
+// A wavefront takes `tokens` rows at a time: as many as have 64 pieces together (30000 rows of 96 channels 4.7 us; one row at a time 9.4).
 template <typename T, bool PAIRS>
 __global__ __launch_bounds__(kWaves * 64) void rotary_kernel(Args a) {
     constexpr uint32_t kEs = (uint32_t)sizeof(T);
-    __shared__ __align__(16) float table[kWaves][kMostD];                          // a wavefront's own: D / 2 cosines, then as many sines
+    __shared__ __align__(16) float table[kWaves][kAngles * 2];                     // a wavefront's own: cosines, then as many sines
     const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = a.D / 2;
-    float *cosine = table[wave], *sine = cosine + half;
-    for (uint64_t row0 = (uint64_t)blockIdx.x * kWaves; row0 < a.rows; row0 += (uint64_t)gridDim.x * kWaves) {
-        const uint64_t row = row0 + wave;
-        const bool live = row < a.rows;
-        __syncthreads();                                 // the last row's angles are read
-        if (live)
-            for (uint32_t i = lane; i < half; i += 64) {
-                double t = 0.0;
-                for (uint32_t x = 0; x < a.axes; ++x) t = __builtin_fma((double)a.pos[row * a.axes + x], (double)a.freq[x * half + i], t);
-                t *= 0.15915494309189533577;             // turns
-                float c, s;
-                turn_of(t, c, s);
-                cosine[i] = c;
-                sine[i] = a.sign * s;
-            }
+    float *cosine = table[wave], *sine = cosine + kAngles;
+    const uint64_t step = (uint64_t)gridDim.x * kWaves * a.tokens;
+    for (uint64_t row0 = (uint64_t)blockIdx.x * kWaves * a.tokens; row0 < a.rows; row0 += step) {
+        const uint64_t first = row0 + (uint64_t)wave * a.tokens;
+        const uint32_t here = first >= a.rows ? 0u : a.rows - first < a.tokens ? (uint32_t)(a.rows - first) : a.tokens;
+        __syncthreads();                                 // the last rows' angles are read
+        for (uint32_t i = lane; i < here * half; i += 64) {
+            const uint32_t token = (uint32_t)divide((int)i, a.per_half), pair = i - token * half;
+            const long long *pos = a.pos + (first + token) * a.axes;
+            double t = 0.0;
+            for (uint32_t x = 0; x < a.axes; ++x) t = __builtin_fma((double)pos[x], (double)a.freq[x * half + pair], t);
+            t *= 0.15915494309189533577;                 // turns
+            float c, s;
+            turn_of(t, c, s);
+            cosine[i] = c;
+            sine[i] = a.sign * s;
+        }
         __syncthreads();
-        if (!live) continue;
-        const unsigned char *xr = a.x + row * a.units * 16 * kEs;
-        unsigned char *yr = a.y + row * a.units * 16 * kEs;
-        for (uint32_t u = lane; u < a.units; u += 64) {
+        const unsigned char *xr = a.x + first * a.units * 16 * kEs;                // the rows lie one behind another
+        unsigned char *yr = a.y + first * a.units * 16 * kEs;
+        for (uint32_t i = lane; i < here * a.units; i += 64) {
+            const uint32_t token = a.tokens == 1 ? 0u : (uint32_t)divide((int)i, a.per_row), u = i - token * a.units;
             const uint32_t head = (uint32_t)divide((int)u, a.per_head), piece = u - head * (a.D / 16);
             const bool turns = u < a.turned;
             // the two halves of 8 channels: eight pairs between them, or four in each
-            const uint32_t lo = PAIRS || !turns ? u * 16 : head * a.D + piece * 8, hi = PAIRS || !turns ? lo + 8 : lo + half;
+            const uint32_t lo = (PAIRS || !turns ? u * 16 : head * a.D + piece * 8) + token * a.units * 16, hi = PAIRS || !turns ? lo + 8 : lo + half;
             rows::Eight<T> p, q;
-            p.load(xr + lo * kEs);
-            q.load(xr + hi * kEs);
+            p.load(xr + (uint64_t)lo * kEs);
+            q.load(xr + (uint64_t)hi * kEs);
             if (turns) {
                 float v[8], w[8], o[8], n[8], c[8], s[8];
                 p.to(v);
                 q.to(w);
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
-                    const f32x4 ct = *reinterpret_cast<const f32x4 *>(cosine + piece * 8 + e), st = *reinterpret_cast<const f32x4 *>(sine + piece * 8 + e);
+                    const f32x4 ct = *reinterpret_cast<const f32x4 *>(cosine + token * half + piece * 8 + e);
+                    const f32x4 st = *reinterpret_cast<const f32x4 *>(sine + token * half + piece * 8 + e);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) { c[e + j] = ct[j]; s[e + j] = st[j]; }
                 }
@@ -96,11 +103,11 @@ __global__ __launch_bounds__(kWaves * 64) void rotary_kernel(Args a) {
                         n[e] = v[e] * s[e] + w[e] * c[e];
                     }
                 }
-                rows::Eight<T>::store(yr + lo * kEs, o);
-                rows::Eight<T>::store(yr + hi * kEs, n);
+                rows::Eight<T>::store(yr + (uint64_t)lo * kEs, o);
+                rows::Eight<T>::store(yr + (uint64_t)hi * kEs, n);
             } else {
-                *reinterpret_cast<rows::Eight<T> *>(yr + lo * kEs) = p;            // bit for bit
-                *reinterpret_cast<rows::Eight<T> *>(yr + hi * kEs) = q;
+                *reinterpret_cast<rows::Eight<T> *>(yr + (uint64_t)lo * kEs) = p;  // bit for bit
+                *reinterpret_cast<rows::Eight<T> *>(yr + (uint64_t)hi * kEs) = q;
             }
         }
     }
@@ -126,9 +133,10 @@ hipError_t launch_rotary(const void *x, const void *pos, void *y, const float *f
     a.x = static_cast<const unsigned char *>(x); a.y = static_cast<unsigned char *>(y); a.pos = static_cast<const long long *>(pos); a.freq = freq;
     a.rows = (uint32_t)rows; a.axes = (uint32_t)axes; a.D = (uint32_t)(channels / (heads + rest));
     a.turned = (uint32_t)heads * (a.D / 16); a.units = (uint32_t)channels / 16;
-    a.per_head = make_divisor(a.D / 16);
+    a.tokens = a.units >= 64 ? 1 : 64 / a.units;         // of at most 64 pieces, half of each rotated: 512 angles at most
+    a.per_head = make_divisor(a.D / 16); a.per_half = make_divisor(a.D / 2); a.per_row = make_divisor(a.units);
     a.sign = backward ? -1.f : 1.f;
-    const long long groups = (rows + rot::kWaves - 1) / rot::kWaves;
+    const long long groups = (rows + rot::kWaves * a.tokens - 1) / (rot::kWaves * a.tokens);
     auto run = [&](auto kernel) { kernel<<<dim3((unsigned)(groups < 16384 ? groups : 16384)), dim3(rot::kWaves * 64), 0, stream>>>(a); };
     if (bf16) { if (pairs) run(rot::rotary_kernel<rows::bf16, true>); else run(rot::rotary_kernel<rows::bf16, false>); }
     else { if (pairs) run(rot::rotary_kernel<float, true>); else run(rot::rotary_kernel<float, false>); }

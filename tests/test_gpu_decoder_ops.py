@@ -26,7 +26,8 @@ def near(got, ref, tol):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M,C,res,add,pack", [(1, 8, False, False, 0), (3, 40, True, True, 1), (77, 768, True, True, 2), (5, 1000, False, True, 1), (130, 512, True, False, 0),
                                               (9, 2048, True, True, 1), (9, 2056, True, True, 2), (4, 8192, True, True, 1), (2100, 64, False, False, 2), (7, 4104, False, False, 0),
-                                              (3, 1544, True, False, 2)])
+                                              (3, 1544, True, False, 2),
+                                              (128, 96, True, True, 1), (16, 1024, False, True, 0), (129, 64, True, True, 0), (2, 8192, False, False, 1)])
 def test_rmsnorm(torch_mod, dtype, M, C, res, add, pack):
     print("rmsnorm", dtype, M, C, res, add, pack, flush=True)
     import paper_2203_15980_amd as dl
