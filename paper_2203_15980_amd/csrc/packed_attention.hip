@@ -34,7 +34,7 @@ __global__ __launch_bounds__(W * G * 64, 2) void forward_kernel(Args a) {
     int head, slot;
     place_of<CAUSAL>(blockIdx.x, gridDim.x, a.heads, a.slots, head, slot);
     Rows r;
-    if (!find_rows<Q>(a, slot, r)) return;
+    if (!find_rows<Q, CAUSAL>(a, a.slots, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
     const int q0 = r.tile * Q;
     unsigned char *yb = a.y + (size_t)r.start * out_pitch + (size_t)head * D * 2;

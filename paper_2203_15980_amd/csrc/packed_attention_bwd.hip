@@ -28,7 +28,7 @@ __device__ __forceinline__ void gq_tile(const Args &a, unsigned block, unsigned 
     int head, slot;
     place_of<CAUSAL>(block, blocks_of_launch, a.heads, a.slots, head, slot);
     Rows r;
-    if (!find_rows<Q>(a, slot, r)) return;
+    if (!find_rows<Q, CAUSAL>(a, a.slots, slot, r)) return;
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
     const int q0 = r.tile * Q;
     unsigned char *gxb = a.gx + (size_t)r.start * pitch + (size_t)head * D * 2;
@@ -153,7 +153,7 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
     place_of<CAUSAL>(workgroup, workgroups, a.kv * a.splits, a.slots, unit, slot);
     const int kh = unit / a.splits, split = unit % a.splits;
     Rows r;
-    if (!find_rows<K>(a, slot, r)) return;
+    if (!find_rows<K, CAUSAL>(a, a.slots, slot, r)) return;
     if (CAUSAL) r.tile = (r.len - 1) / K - r.tile;       // a sequence's first keys have the most queries
     const size_t out_pitch = (size_t)a.heads * D * 2, pitch = (size_t)(a.heads + 2 * a.kv) * D * 2;
     const int first = r.tile * K, share = a.heads / a.kv / a.splits;                // query heads of this workgroup
