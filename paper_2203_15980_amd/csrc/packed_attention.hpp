@@ -184,7 +184,7 @@ struct Loader {
         lds = wave * kRows * D * 2;
     }
     __device__ __forceinline__ void load(const unsigned char *base, uint32_t pitch, int rows, uint32_t tile) const {
-#pragma unroll kTurns > 4 ? 2 : kTurns
+#pragma unroll W < 4 && kTurns > 2 ? 2 : kTurns
         for (int t = 0; t < kTurns; ++t) {
             const int r = row + t * kRows * W;
             const uint32_t piece = (uint32_t)(((int)(threadIdx.x & 63) % (D / 8)) ^ twist<D>(r)) * 16;

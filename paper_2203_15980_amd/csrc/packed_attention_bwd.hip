@@ -194,14 +194,18 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
         for (int e = 0; e < 16; ++e) gk[t][e] = gv[t][e] = 0.f;
     const int begin = CAUSAL ? first / Q : 0, per = (r.len + Q - 1) / Q - begin;
     const Loader<D, W, Q> loader(wave);
-    float st = 0.f;                                      // the thread's statistic of the block on its way: log-sum-exp (the first Q threads), delta (the next Q)
+    float lse2 = 0.f, delta = 0.f;                       // of the block on its way, query `thread`
+    static_assert(Q <= W * 64, "a query to a thread");
     auto load = [&](int head, int at, int buffer) {
         const uint32_t to = lds + (uint32_t)buffer * 2 * kTile<D, Q>;
         loader.load(xb + (size_t)at * pitch + (size_t)head * D * 2, (uint32_t)pitch, r.len - at, to);
         loader.load(a.gy + ((size_t)r.start + at) * out_pitch + (size_t)head * D * 2, (uint32_t)out_pitch, r.len - at, to + kTile<D, Q>);
-        const int q = at + (thread & (Q - 1));
-        if (thread < Q) st = q < r.len ? a.lse[(size_t)head * a.M + r.start + q] * kLog2e : __builtin_inff();      // p = 0 behind the last query
-        else if (!OWN && thread < 2 * Q) st = q < r.len ? a.delta[(size_t)head * a.M + r.start + q] : 0.f;
+        if (thread < Q) {
+            const int q = at + thread;
+            const size_t stat = (size_t)head * a.M + r.start + q;
+            lse2 = q < r.len ? a.lse[stat] * kLog2e : __builtin_inff();            // p = 0 behind the last query
+            if (!OWN) delta = q < r.len ? a.delta[stat] : 0.f;
+        }
     };
     // Each head's queries from the last block on backwards: causal, workgroups on an XCD begin at the same block and find it in its L2.  The groups take turns at the
     // blocks of all heads in one row.
@@ -238,7 +242,10 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
         }
     }
     for (int i = 0; i * G < per * share; ++i) {
-        if (thread < 2 * Q) stats[group][buffer][thread / Q][thread & (Q - 1)] = st;
+        if (thread < Q) {
+            stats[group][buffer][0][thread] = lse2;
+            if (!OWN) stats[group][buffer][1][thread] = delta;
+        }
         arrived();
         __syncthreads();                                 // the block is there; the one before is done with
         const int at = (begin + block) * Q;

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kWaves * 64) void rotary_kernel(Args a) {
 
 // `heads` rotated heads and `rest` copied ones, of D channels: channels = (heads + rest) D.
 const char *rotary_check(const float *freq, long long rows, int channels, int heads, int rest, long long axes) {
-    if (heads <= 0 || rest < 0 || channels % (heads + rest)) return "rotary positions need R rotated heads and S others, (R + S) D channels";
+    if (heads <= 0 || rest < 0 || heads > channels || rest > channels - heads || channels % (heads + rest)) return "rotary positions need R rotated heads and S others, (R + S) D channels";
     const int D = channels / (heads + rest);
     if (D % 16 || D > rot::kMostD) return "rotary positions need heads of a multiple of 16 channels, up to 256";
     if (axes < 1 || axes > rot::kMostAxes) return "positions must hold 1 to 8 int64 values for each row";

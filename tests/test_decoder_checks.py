@@ -27,7 +27,7 @@ def test_rmsnorm_check(gamma, rows, C_, why):
 @pytest.mark.parametrize("freq,rows,channels,heads,rest,axes,why", [
     (4, 1, 64, 1, 0, 1, ""), (4, 9, 480, 4, 2, 8, ""), (4, 1, 256, 1, 0, 3, ""), (0, 1, 64, 1, 0, 1, "scale"), (4, 1, 64, 0, 1, 1, "R rotated"), (4, 1, 64, 1, -1, 1, "R rotated"),
     (4, 1, 65, 2, 0, 1, "R rotated"), (4, 1, 48, 2, 0, 1, "16 channels"), (4, 1, 272, 1, 0, 1, "256"), (4, 1, 64, 1, 0, 0, "1 to 8"), (4, 1, 64, 1, 0, 9, "1 to 8"),
-    (4, 2 ** 31, 64, 1, 0, 1, "rows")])
+    (4, 2 ** 31, 64, 1, 0, 1, "rows"), (4, 1, 64, 2 ** 31 - 1, 2 ** 31 - 1, 1, "R rotated"), (4, 1, 64, 2 ** 30, 2 ** 30, 1, "R rotated")])
 def test_rotary_check(freq, rows, channels, heads, rest, axes, why):
     got = check(ROT, P(freq), LL(rows), I(channels), I(heads), I(rest), LL(axes))
     assert (why in got) if why else not got
@@ -36,7 +36,8 @@ def test_rotary_check(freq, rows, channels, heads, rest, axes, why):
 @pytest.mark.parametrize("M,seqs,cin,cout,heads,kv,bf16,why", [
     (1, 1, 192, 64, 1, 1, 1, ""), (8192, 64, 6144, 4096, 32, 8, 1, ""), (1, 1, 192, 64, 1, 1, 0, "bf16"), (1, 1, 192, 64, 0, 1, 1, "R query heads"), (1, 1, 320, 192, 3, 2, 1, "multiple of S"),
     (1, 1, 96, 32, 1, 1, 1, "64 or 128"), (1, 1, 768, 256, 1, 1, 1, "64 or 128"), (1, 1, 200, 64, 1, 1, 1, "Cin"), (0, 1, 192, 64, 1, 1, 1, "rows"), (1, 0, 192, 64, 1, 1, 1, "offsets"),
-    (2 ** 30, 1, 192, 64, 1, 1, 1, "too many"), (1000, 2 ** 24, 192, 64, 1, 1, 1, "too many")])
+    (2 ** 30, 1, 192, 64, 1, 1, 1, "too many"), (1000, 2 ** 24, 192, 64, 1, 1, 1, "too many"), (9, 1, 3 * 2 ** 23, 2 ** 23, 2 ** 16, 2 ** 16, 1, "16777216 channels"),
+    (9, 1, 64 * 9, 64 * 3, 2 ** 30, 2 ** 30, 1, "64 or 128")])
 def test_packed_attention_check(M, seqs, cin, cout, heads, kv, bf16, why):
     got = check(ATT, LL(M), LL(seqs), I(cin), I(cout), I(heads), I(kv), I(bf16))
     assert (why in got) if why else not got
@@ -47,6 +48,24 @@ def test_packed_attention_check(M, seqs, cin, cout, heads, kv, bf16, why):
 def test_logprob_check(rows, V, K, why):
     got = check(LPR, LL(rows), I(V), I(K))
     assert (why in got) if why else not got
+
+
+def test_decoder_kernels_use_no_private_memory(tmp_path):
+    """What they work on stays in registers and LDS, as the built library's code objects declare it."""
+    import os
+    import re
+    import subprocess
+    llvm = "/opt/rocm/lib/llvm/bin/"
+    os.symlink(os.path.join(os.path.dirname(os.path.abspath(dl.__file__)), "libdelta.so"), str(tmp_path / "lib.so"))
+    subprocess.run([llvm + "llvm-objdump", "--offloading", str(tmp_path / "lib.so")], cwd=str(tmp_path), check=True, stdout=subprocess.DEVNULL)
+    private = {}
+    for name in sorted(os.listdir(str(tmp_path))):
+        if "gfx950" in name:
+            notes = subprocess.run([llvm + "llvm-readelf", "--notes", str(tmp_path / name)], check=True, stdout=subprocess.PIPE).stdout.decode()
+            for kernel, n in re.findall(r"\.name:\s+(\S+)\n(?:(?!\.name:).)*?\.private_segment_fixed_size:\s+(\d+)", notes, re.S):
+                if any(s in kernel for s in ("N5delta3rms", "N5delta3rot", "N5delta3pat", "N5delta3lpr")):
+                    private[kernel] = int(n)
+    assert len(private) >= 60 and not {k: v for k, v in private.items() if v}
 
 
 def slots_and_tiles(off, M, Q):

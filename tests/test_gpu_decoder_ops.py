@@ -183,6 +183,25 @@ def test_attention_of_many_sequences(torch_mod, n, most):
     b.close()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("seqs,most,heads,kv,D", [(60, 300, 8, 2, 64), (62, 150, 8, 8, 128), (63, 150, 8, 8, 128), (3, 600, 12, 4, 64), (2, 500, 12, 12, 128), (100, 60, 16, 2, 64), (1, 1100, 12, 3, 64)])
+def test_attention_where_the_chip_is_full(torch_mod, causal, seqs, most, heads, kv, D):
+    """Launches of one and two groups of wavefronts to a tile, of both gradients apart, and of more sequences than a wavefront has lanes."""
+    print("attention", causal, seqs, most, heads, kv, D, flush=True)
+    rng = np.random.default_rng(seqs + most)
+    lens = rng.integers(0, most + 1, seqs)
+    lens[-1] = most
+    off = offsets(lens, 3)
+    M = int(off[-1]) + 70
+    x, gy = storage(rng.normal(size=(M, (heads + 2 * kv) * D)), "bf16"), storage(rng.normal(size=(M, heads * D)), "bf16")
+    b, o = run_attention(torch_mod, x, off, heads, kv, D, causal, gy)
+    alone = np.r_[0:3, off[-1]:M]
+    assert not o["y"][alone].any() and not o["lse"][:, alone].any() and not o["gx"][alone].any()
+    check_attention(o, od.attention(values(x, "bf16"), off, heads, kv, D, causal, values(gy, "bf16")), heads, D, most)
+    assert b.untouched()
+    b.close()
+
+
 @pytest.mark.parametrize("size", [1e-3, 8.0, 40.0])
 def test_attention_with_flat_and_sharp_scores(torch_mod, size):
     """Scores of almost no spread, and of some thousand units: a single key has all the weight."""
