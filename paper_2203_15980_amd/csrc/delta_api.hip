@@ -1526,10 +1526,10 @@ delta_status prepare_backward_rows(delta_ctx *c, const delta_bwd_desc &D, uint32
 }
 
 // A decoder layer's operators.  Workspace: root-mean-square normalisation's for gw, attention's for gx.
-uint64_t decoder_workspace_bytes(const delta_layer_desc &L) {
+uint64_t decoder_workspace_bytes(delta_ctx *c, const delta_layer_desc &L) {
     const long long rows = (long long)L.N * L.H * L.W;
     const uint64_t need = L.op == DELTA_OP_RMSNORM ? delta::rmsnorm_bwd_workspace_bytes(rows, L.Cin)
-                          : L.op == DELTA_OP_ATTENTION_PACKED ? delta::packed_attention_bwd_workspace_bytes(rows, L.Cout, L.R, L.S) : 0;
+                          : L.op == DELTA_OP_ATTENTION_PACKED ? delta::packed_attention_bwd_workspace_bytes(rows, (long long)(c->tensors[L.res].bytes / 8) - 1, L.Cout, L.R, L.S) : 0;
     return (need + 255) / 256 * 256;
 }
 // What the gradient reads beside gy and gx_add: `n` ids.
@@ -1568,7 +1568,7 @@ delta_status prepare_backward_decoder(delta_ctx *c, const delta_bwd_desc &D, uin
     }
     if (D.gw && ((uintptr_t)D.gw & 15)) return fail(c, DELTA_ERR_INVALID, "backward %u: gw misaligned", i);
     if ((D.gw || L.op == DELTA_OP_ATTENTION_PACKED) &&
-        (!D.workspace || ((uintptr_t)D.workspace & 255) || D.workspace_bytes < decoder_workspace_bytes(L)))
+        (!D.workspace || ((uintptr_t)D.workspace & 255) || D.workspace_bytes < decoder_workspace_bytes(c, L)))
         return fail(c, DELTA_ERR_INVALID, "backward %u: workspace missing, not 256-byte aligned or too small", i);
     return DELTA_OK;
 }
@@ -1874,7 +1874,7 @@ delta_status delta_backward_workspace(delta_ctx *c, const delta_layer_desc *laye
         *out_bytes = row_op_workspace_bytes(*layer);
         return DELTA_OK;
     }
-    if (decoder_op(*layer)) { *out_bytes = decoder_workspace_bytes(*layer); return DELTA_OK; }
+    if (decoder_op(*layer)) { *out_bytes = decoder_workspace_bytes(c, *layer); return DELTA_OK; }
     if (layer->op != DELTA_OP_CONV) { *out_bytes = 0; return DELTA_OK; }
     if (is_stem(*layer)) { *out_bytes = delta::stem_wgrad_workspace_bytes(a); return DELTA_OK; }
     as_stride_1(*layer, a);
@@ -2039,7 +2039,7 @@ delta_status delta_backward_segment(delta_ctx *c, const delta_bwd_desc *descs, u
                 gxp = c->arena + c->tensors[D.gx].offset;
             }
             // as for the row operators: the end of the workspace
-            const uint64_t need = D.gw || L.op == DELTA_OP_ATTENTION_PACKED ? decoder_workspace_bytes(L) : 0;
+            const uint64_t need = D.gw || L.op == DELTA_OP_ATTENTION_PACKED ? decoder_workspace_bytes(c, L) : 0;
             unsigned char *work = need ? static_cast<unsigned char *>(D.workspace) + ((D.workspace_bytes - need) & ~(uint64_t)255) : nullptr;
             if (need && aux_holds(c, work, need) && (r = join_aux(c)) != DELTA_OK) return r;
             const long long rows = (long long)L.N * L.H * L.W;

@@ -189,7 +189,7 @@ hipError_t launch_rotary(const void *x, const void *pos, void *y, const float *f
 const char *packed_attention_check(long long M, long long seqs, int Cin, int Cout, int heads, int kv, int bf16);
 hipError_t launch_packed_attention(const void *x, const void *off, void *y, float *lse, long long M, long long seqs, int Cin, int Cout, int heads, int kv,
                                    int causal, int bf16, hipStream_t stream);
-size_t packed_attention_bwd_workspace_bytes(long long M, int Cout, int heads, int kv);
+size_t packed_attention_bwd_workspace_bytes(long long M, long long seqs, int Cout, int heads, int kv);
 hipError_t launch_packed_attention_bwd(const void *x, const void *off, const void *y, const float *lse, const void *gy, void *gx, long long M, long long seqs,
                                        int Cin, int Cout, int heads, int kv, int causal, int bf16, void *workspace, size_t workspace_bytes, hipStream_t stream);
 // logprob.hip: log probabilities of given tokens, entropy, log-sum-exp, most likely tokens; gradients

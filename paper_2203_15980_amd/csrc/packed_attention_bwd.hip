@@ -415,11 +415,19 @@ static hipError_t backward(const Args &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// In how many shares a key head's query heads go: as few as give the chip two rounds of its 512 workgroups.
-static int splits_of(long long M, int heads, int kv) {
+// In how many shares a key head's query heads go: as few as give the chip two rounds of its 512 workgroups; of short sequences, where a workgroup has little to do and the
+// parts' trip through memory counts for more, half a round.  us of the gradients with 1, 2, 4 and 8 shares (as many as there are query heads), causal:
+//   8192 tokens, 32 heads over 8 of 128                     2427, 1798, 1836
+//   2048 tokens, 8 heads over 1 of 128                      278, 166, 110, 89
+//   9 sequences of up to 1531, 16 heads over 2 of 128       416, 236, 227, 181
+//   1 x 512, 4 heads over 1 of 64                           28, 21, 15
+//   64 sequences of up to 120, 16 heads over 4 of 128       78, 76, 90
+//   100 sequences of up to 80, 32 heads over 4 of 64        62, 71, 78, 92
+static int splits_of(long long M, long long seqs, int heads, int kv) {
     const int group = heads / kv;
+    const long long tiles = (M + 127) / 128, want = M >= 512 * seqs ? 1024 : 256, there = M >= 512 * seqs ? tiles : tiles + seqs;
     int n = 1;
-    while (n < group && (group % n || (M + 127) / 128 * kv * n < 1024)) ++n;
+    while (n < group && (group % n || there * kv * n < want)) ++n;
     return n;
 }
 
@@ -427,8 +435,8 @@ static int splits_of(long long M, int heads, int kv) {
 
 // delta, and behind it the parts of gk and gv where there are several.
 static size_t delta_bytes(long long M, int heads) { return ((size_t)M * heads * sizeof(float) + 255) / 256 * 256; }
-size_t packed_attention_bwd_workspace_bytes(long long M, int Cout, int heads, int kv) {
-    const int n = pat::splits_of(M, heads, kv);
+size_t packed_attention_bwd_workspace_bytes(long long M, long long seqs, int Cout, int heads, int kv) {
+    const int n = pat::splits_of(M, seqs, heads, kv);
     return delta_bytes(M, heads) + (n > 1 ? (size_t)n * M * 2 * kv * (Cout / heads) * sizeof(float) : 0);
 }
 
@@ -436,13 +444,13 @@ size_t packed_attention_bwd_workspace_bytes(long long M, int Cout, int heads, in
 hipError_t launch_packed_attention_bwd(const void *x, const void *off, const void *y, const float *lse, const void *gy, void *gx, long long M, long long seqs,
                                        int Cin, int Cout, int heads, int kv, int causal, int bf16, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     if (!x || !off || !y || !lse || !gy || !gx || packed_attention_check(M, seqs, Cin, Cout, heads, kv, bf16)) return hipErrorInvalidValue;
-    if (!workspace || workspace_bytes < packed_attention_bwd_workspace_bytes(M, Cout, heads, kv)) return hipErrorInvalidValue;
+    if (!workspace || workspace_bytes < packed_attention_bwd_workspace_bytes(M, seqs, Cout, heads, kv)) return hipErrorInvalidValue;
     pat::Args a = {};
     a.x = static_cast<const unsigned char *>(x); a.off = static_cast<const long long *>(off);
     a.y = static_cast<unsigned char *>(const_cast<void *>(y)); a.lse = const_cast<float *>(lse);
     a.gy = static_cast<const unsigned char *>(gy); a.gx = static_cast<unsigned char *>(gx); a.delta = static_cast<float *>(workspace);
     a.M = (int)M; a.seqs = (int)seqs; a.heads = heads; a.kv = kv;
-    a.splits = pat::splits_of(M, heads, kv);
+    a.splits = pat::splits_of(M, seqs, heads, kv);
     a.part = a.splits > 1 ? reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + delta_bytes(M, heads)) : nullptr;
     a.scale = 1.0f / sqrtf((float)(Cout / heads));
     a.scale_log2e = a.scale * pat::kLog2e;
