@@ -7,7 +7,9 @@
 // r comes from s again in the backward pass, as in layernorm.hip: nothing but s has to be kept.
 //
 // Bound by memory: forward with residual and checkpoint 9.03 bytes a value in bf16, backward with gx_add 8.  A wavefront owns a row up to 2048 channels, a
-// workgroup beyond (eight channels a thread); the row stays in registers from its load to its store.
+// workgroup beyond (eight channels a thread); the row stays in registers from its load to its store.  us, rows one after another from HBM: 8192 x 4096 in bf16
+// forward with residual and int8 checkpoint 52 (303 MB, 5.8 TB/s), gradients with gx_add 46 (268 MB, 5.8 TB/s); fp32 forward 107 (5.3 TB/s), gradients 101
+// (5.3 TB/s); 16384 x 768 in bf16 forward 16, gradients 22 (their operands partly from the shared cache); 77 x 768 3.4 and 6.3: launches.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -386,9 +388,11 @@ __global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor pe
 // us with gx_add, bf16: 1 x 4096 3.8, 128 x 64 4.1, two launches 6.2 whatever the size up to 77 x 768, which takes 7.0 like this: a workgroup reads everything.
 constexpr bool few_rows(uint64_t rows, uint64_t C) { return rows <= kFew && rows * C <= kFewValues && C % 32 == 0; }
 
-// Workgroups of the backward launch, a partial sum of dgamma to each.
+// Workgroups of the backward launch, a partial sum of dgamma to each.  A row to a workgroup: two at least, whose loads go out together, and the partial sums are half as many (us
+// with one, two and four: 300 x 8192 17.0, 12.1, 12.6; 500 x 4096 13.9, 10.6, 10.3; 1032 x 3080 in fp32 17.3, 17.2, 17.9).  A row to a wavefront: one (1000 x 2048 7.9,
+// 9.4, 13.6).
 uint32_t workgroups(long long rows, int C) {
-    const long long per = C <= kWaveChannels ? 8 : 1, most = C <= kWaveChannels ? 256 : 512;
+    const long long per = C <= kWaveChannels ? 8 : 2, most = C <= kWaveChannels ? 256 : 512;
     const long long want = (rows + per - 1) / per;
     return (uint32_t)(want < most ? want : most);
 }
