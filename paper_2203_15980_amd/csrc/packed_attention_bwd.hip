@@ -136,14 +136,14 @@ __device__ __forceinline__ void gq_tile(const Args &a, unsigned block, unsigned 
 
 // Heads of 128: a lane's sums of gk and gv, its key and its value would be 192 registers of the 256 that two wavefronts to a SIMD leave: the values stay in LDS, and
 // with them (32 KB) and another workgroup's there is room for blocks of 32 queries.
-template <int D> constexpr int kQueries = D == 128 ? 32 : 64;
-template <int D, int W, int G> constexpr int kKvLds = G * 4 * kTile<D, kQueries<D>> + (D == 128 ? kTile<D, W * 32> : 0);
+template <int D, int W> constexpr int kQueries = D == 128 && W < 8 ? 32 : 64;
+template <int D, int W, int G> constexpr int kKvLds = G * 4 * kTile<D, kQueries<D, W>> + (D == 128 ? kTile<D, W * 32> : 0);
 
 // OWN: with delta made here, for all queries that the keys may meet, instead of read: both kernels are one launch then.
 constexpr int kOwn = 2048;
 template <int D, int W, int G, bool CAUSAL, bool OWN>
 __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsigned workgroups, unsigned char *smem) {
-    constexpr int K = W * 32, KS = D / 16, DB = D / 32, Q = kQueries<D>;
+    constexpr int K = W * 32, KS = D / 16, DB = D / 32, Q = kQueries<D, W>;
     constexpr bool kValuesInLds = D == 128;
     __shared__ __align__(16) float own[OWN ? kOwn : 4];  // [head of the share][query, to whole blocks]
     __shared__ __align__(16) float stats[G][2][2][Q];    // of a block's queries: log-sum-exp (log2), delta
@@ -255,7 +255,7 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
         if (head < end) load(head, (begin + block) * Q, buffer ^ 1);
         const unsigned char *qs = tiles + buffer * 2 * kTile<D, Q>, *gs = qs + kTile<D, Q>;
         if (some && w0 < r.len && (!CAUSAL || at + Q - 1 >= w0)) {
-#pragma unroll
+#pragma unroll D == 128 && CAUSAL ? 1 : 2
             for (int t = 0; t < Q / 32; ++t) {
                 __builtin_amdgcn_sched_barrier(0);       // one tile after the other
                 f32x16 s, dp;
@@ -287,6 +287,7 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
                     }
                     asm volatile("" ::: "memory");
                 }
+                if (D == 128) __builtin_amdgcn_sched_barrier(0);                   // nor the products' operands before the weights are bf16
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const bf16x8 p = as_operand(s, j), ds = as_operand(dp, j);
@@ -406,7 +407,7 @@ static hipError_t backward(const Args &a, hipStream_t stream) {
     } else {
         e = gq == 4 ? launch_gq<D, 1, 4, CAUSAL>(a, stream) : gq == 2 ? launch_gq<D, 2, 2, CAUSAL>(a, stream) : launch_gq<D, 4, 1, CAUSAL>(a, stream);
         if (e != hipSuccess) return e;
-        e = gkv == 4 ? launch_gkv<D, 1, 4, CAUSAL>(a, stream) : gkv == 2 ? launch_gkv<D, 2, 2, CAUSAL>(a, stream) : launch_gkv<D, 4, 1, CAUSAL>(a, stream);
+        e = gkv == 4 ? launch_gkv<D, 1, 4, CAUSAL>(a, stream) : gkv == 2 ? launch_gkv<D, 2, 2, CAUSAL>(a, stream) : launch_gkv<D, D == 128 ? 8 : 4, 1, CAUSAL>(a, stream);
     }
     if (e != hipSuccess || a.splits == 1) return e;
     const uint32_t n = (uint32_t)(2 * a.kv * D);
