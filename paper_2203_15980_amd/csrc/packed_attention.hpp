@@ -23,7 +23,7 @@ struct Args {
     float *lse;                                          // [heads][M], natural; null: not stored
     const unsigned char *gy;                             // [M][heads D]
     unsigned char *gx;                                   // as x
-    float *delta;                                        // [heads][M], sum over a row's channels of y gy
+    float *delta;                                        // [heads][M], sum over a row's channels of y gy; then [heads][M] log2-sum-exp
     float *part;                                         // null or [splits][M][2 kv D]: sums of gk and gv over a share of a key head's query heads
     int M, seqs, heads, kv, slots, splits;
     float scale, scale_log2e;                            // 1 / sqrt(D), times log2 e

@@ -64,7 +64,10 @@ __device__ __forceinline__ void gq_tile(const Args &a, unsigned block, unsigned 
     delta = rows::halves(delta);
     const size_t stat = (size_t)head * a.M + r.start + row;
     const float lse2 = a.lse[stat] * kLog2e;
-    if (there && !half && !group) a.delta[stat] = delta;
+    if (there && !half && !group) {
+        a.delta[stat] = delta;
+        a.delta[(size_t)a.heads * a.M + stat] = lse2;
+    }
     f32x16 g[DB];
 #pragma unroll
     for (int t = 0; t < DB; ++t)
@@ -194,17 +197,23 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
         for (int e = 0; e < 16; ++e) gk[t][e] = gv[t][e] = 0.f;
     const int begin = CAUSAL ? first / Q : 0, per = (r.len + Q - 1) / Q - begin;
     const Loader<D, W, Q> loader(wave);
-    float lse2 = 0.f, delta = 0.f;                       // of the block on its way, query `thread`
+    const uint32_t lds_stats = lds_of(reinterpret_cast<const unsigned char *>(&stats[group][0][0][0]));
+    float lse2 = 0.f;                                    // OWN: of the block on its way, query `thread`
     static_assert(Q <= W * 64, "a query to a thread");
     auto load = [&](int head, int at, int buffer) {
         const uint32_t to = lds + (uint32_t)buffer * 2 * kTile<D, Q>;
         loader.load(xb + (size_t)at * pitch + (size_t)head * D * 2, (uint32_t)pitch, r.len - at, to);
         loader.load(a.gy + ((size_t)r.start + at) * out_pitch + (size_t)head * D * 2, (uint32_t)out_pitch, r.len - at, to + kTile<D, Q>);
-        if (thread < Q) {
-            const int q = at + thread;
-            const size_t stat = (size_t)head * a.M + r.start + q;
-            lse2 = q < r.len ? a.lse[stat] * kLog2e : __builtin_inff();            // p = 0 behind the last query
-            if (!OWN) delta = q < r.len ? a.delta[stat] : 0.f;
+        if constexpr (OWN) {
+            if (thread < Q) lse2 = a.lse[(size_t)head * a.M + r.start + (at + thread < r.len ? at + thread : r.len - 1)] * kLog2e;
+        } else {                                         // 64 numbers to a wavefront's load: the log-sum-exps, then the deltas, of Q queries
+#pragma unroll
+            for (int part = 0; part < 2 * Q / 64; ++part)
+                if (wave == part % W) {
+                    const int i = part * 64 + lane, q = at + i % Q;
+                    const float *from = a.delta + (i < Q ? (size_t)a.heads * a.M : 0) + (size_t)head * a.M + r.start + (q < r.len ? q : r.len - 1);
+                    load_lds_b32(from, lds_stats + (uint32_t)(buffer * 2 * Q + part * 64) * 4);
+                }
         }
     };
     // Each head's queries from the last block on backwards: causal, workgroups on an XCD begin at the same block and find it in its L2.  The groups take turns at the
@@ -242,10 +251,7 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
         }
     }
     for (int i = 0; i * G < per * share; ++i) {
-        if (thread < Q) {
-            stats[group][buffer][0][thread] = lse2;
-            if (!OWN) stats[group][buffer][1][thread] = delta;
-        }
+        if (OWN && thread < Q) stats[group][buffer][0][thread] = lse2;
         arrived();
         __syncthreads();                                 // the block is there; the one before is done with
         const int at = (begin + block) * Q;
@@ -255,7 +261,7 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
         if (head < end) load(head, (begin + block) * Q, buffer ^ 1);
         const unsigned char *qs = tiles + buffer * 2 * kTile<D, Q>, *gs = qs + kTile<D, Q>;
         if (some && w0 < r.len && (!CAUSAL || at + Q - 1 >= w0)) {
-#pragma unroll D == 128 && CAUSAL ? 1 : 2
+#pragma unroll D == 128 ? 1 : 2
             for (int t = 0; t < Q / 32; ++t) {
                 __builtin_amdgcn_sched_barrier(0);       // one tile after the other
                 f32x16 s, dp;
@@ -278,12 +284,14 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
                         dp[4 * e4 + e] = p * (dp[4 * e4 + e] - dl[e]);
                     }
                 }
-                if (CAUSAL && __builtin_expect(at + 32 * t < w0 + 31, 0)) {
-                    const int from = key - at - 32 * t - 4 * half;                 // the first row of the product that sees this key
+                if (__builtin_expect((CAUSAL && at + 32 * t < w0 + 31) || at + 32 * t + 32 > r.len, 0)) {
+                    // the rows of the product that see this key: causal from its own on, and queries of the sequence
+                    const int from = CAUSAL ? key - at - 32 * t - 4 * half : -64, to = r.len - at - 32 * t - 4 * half;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        s[e] = row_of(e) >= from ? s[e] : 0.f;
-                        dp[e] = row_of(e) >= from ? dp[e] : 0.f;
+                        const bool sees = row_of(e) >= from && row_of(e) < to;
+                        s[e] = sees ? s[e] : 0.f;
+                        dp[e] = sees ? dp[e] : 0.f;
                     }
                     asm volatile("" ::: "memory");
                 }
@@ -434,8 +442,8 @@ static int splits_of(long long M, long long seqs, int heads, int kv) {
 
 }  // namespace pat
 
-// delta, and behind it the parts of gk and gv where there are several.
-static size_t delta_bytes(long long M, int heads) { return ((size_t)M * heads * sizeof(float) + 255) / 256 * 256; }
+// delta and the log-sum-exp in powers of two, and behind them the parts of gk and gv where there are several.
+static size_t delta_bytes(long long M, int heads) { return ((size_t)M * heads * 2 * sizeof(float) + 255) / 256 * 256; }
 size_t packed_attention_bwd_workspace_bytes(long long M, long long seqs, int Cout, int heads, int kv) {
     const int n = pat::splits_of(M, seqs, heads, kv);
     return delta_bytes(M, heads) + (n > 1 ? (size_t)n * M * 2 * kv * (Cout / heads) * sizeof(float) : 0);
