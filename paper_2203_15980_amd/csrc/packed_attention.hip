@@ -110,7 +110,7 @@ __global__ __launch_bounds__(W * G * 64, 2) void forward_kernel(Args a) {
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[t][e]);
             const float m_new = fmaxf(m_run, halves_max(mx) * a.scale_log2e);
             // Where no lane's maximum grows nothing is scaled.  Scaling later still, once it has grown by 2^8, saved 4 % of long sequences' time, but a row's largest weight is then
-            // not exactly one, and y a third further from 64 bits.
+            // not exactly one, and y 0.0021 instead of 0.0018 from 64 bits.
             if (__any(m_new > m_run)) {
                 const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);         // 0 on the first block
                 m_run = m_new;
