@@ -187,7 +187,7 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * DELTA_OP_EMBEDDING: y[m,k] = scale_k * w[id[m]][k] over m in N*H*W tokens (at most 16777216): x holds their ids, int64, Cin = the rows of
  * the table (at most 4194303), Cout = its channels (a multiple of 8 up to 8192), w = the table [Cin][Cout] in the storage type, bf16 or fp32,
  * scale = a factor per channel (a constant one for the usual sqrt(Cout)).  An id outside [0, Cin) stands for no token: its row of y is zero.
- * A decoder layer's operators (N * H * W rows; y2 and y3 are further outputs, DELTA_NO_TENSOR where there is none):
+ * A decoder layer's operators (N * H * W rows, at most 2147483647; y2 and y3 are further outputs, DELTA_NO_TENSOR where there is none):
  * DELTA_OP_RMSNORM (bf16 and fp32, Cin = Cout a multiple of 8 up to 8192): s = x + res, rounded to the storage type and stored in y2; without res s = x and y2
  * is DELTA_NO_TENSOR.  y = s / sqrt(mean(s^2) + eps) * scale over the channels of each row; scale = gamma (fp32, 16-byte aligned), no shift.  The sum of
  * squares is fp32: finite for |s| up to 2^63 / sqrt(Cin).  With `pack`, y3 receives y's checkpoint, the bits that DELTA_OP_PACK8 makes of y;

@@ -57,6 +57,7 @@ class Event(C.Structure):
 
 
 class LayerDesc(C.Structure):
+    """What is left out is 0: also y2 and y3, which OP_RMSNORM, OP_ROTARY, OP_ATTENTION_PACKED and OP_LOGPROB take as tensor 0 (NO_TENSOR: none)."""
     _fields_ = [("x", C.c_uint32), ("res", C.c_uint32), ("y", C.c_uint32), ("dtype", C.c_uint32),
                 ("w", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p),
                 ("N", C.c_int32), ("H", C.c_int32), ("W", C.c_int32), ("Cin", C.c_int32),

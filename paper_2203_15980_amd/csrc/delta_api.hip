@@ -793,7 +793,11 @@ static delta_status prepare_layer(delta_ctx *c, const delta_layer_desc &L, uint3
                     "layers only", i);
     if (L.flags && !((L.op == DELTA_OP_ATTENTION_PACKED || L.op == DELTA_OP_ROTARY) && L.flags == 1))
         return fail(c, DELTA_ERR_INVALID, "layer %u: unknown flags %u", i, L.flags);
-    if (decoder_op(L)) {                             // the further outputs: tensors of their own
+    if (decoder_op(L)) {
+        const uint64_t images = (uint64_t)L.N * (uint64_t)L.H;
+        if (images > 0x7FFFFFFFull || images * (uint64_t)L.W > 0x7FFFFFFFull)
+            return fail(c, DELTA_ERR_INVALID, "layer %u: this operator takes at most 2147483647 rows", i);
+        // the further outputs: tensors of their own
         const uint32_t ids[5] = {L.x, L.res, L.y, L.y2, L.y3};
         for (int j = 3; j < 5; ++j) {
             if (ids[j] == DELTA_NO_TENSOR) continue;

@@ -302,6 +302,9 @@ def test_refusals_leave_everything_as_it_was(torch_mod):
                dict(y=i["best"]), dict(dtype=7)):
         forward("lp", **kw)
     forward("o", flags=1)                                        # an operator without flags
+    for of in ("n1", "rot", "att", "lp"):                        # rows that wrap around in 64 bits
+        forward(of, N=2 ** 30, H=2 ** 30, W=2)
+        forward(of, N=2 ** 31 - 1, H=2 ** 31 - 1, W=2 ** 31 - 1)
     s.b.d.release(i["pos"], dl.EV_OFFLOAD)
     forward("rot", status=dl.ERR_STATE)
     s.b.d.prefetch(i["pos"])
@@ -351,6 +354,20 @@ def test_an_operator_that_finds_no_room_leaves_none_of_its_outputs_resident(torc
         with pytest.raises(dl.DeltaError):
             d.tensor_ptr(t)
     assert d.stats()["arena_in_use"] == before
+    d.close()
+
+
+def test_rows_that_wrap_around_are_refused_before_bytes_are_divided(torch_mod):
+    """2^61 rows of 8 bytes are 2^64, and so are those of x: a tensor of no bytes has both sizes."""
+    import paper_2203_15980_amd as dl
+    torch = torch_mod
+    arena, f = torch.zeros(4096, dtype=torch.uint8, device="cuda:0"), torch.zeros(64, device="cuda:0")
+    d = dl.Delta(arena, torch.cuda.current_stream().cuda_stream)
+    d.bind([0, 0, 0])
+    with pytest.raises(dl.DeltaError) as e:
+        d.recompute_segment([dl.LayerDesc(x=0, res=1, y=2, y2=dl.NO_TENSOR, y3=dl.NO_TENSOR, dtype=dl.DTYPE_BF16, N=2 ** 30, H=2 ** 30, W=2, Cin=16, Cout=16, R=1, S=0, stride=1,
+                                          op=dl.OP_ROTARY, scale=f.data_ptr())])
+    assert e.value.status == dl.ERR_INVALID and "2147483647 rows" in e.value.message
     d.close()
 
 
