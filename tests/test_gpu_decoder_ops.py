@@ -151,7 +151,7 @@ def offsets(lens, before=0):
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("lens,before,behind,heads,kv,D", [
     ([1], 0, 0, 1, 1, 64), ([77], 0, 0, 12, 12, 64), ([64], 0, 0, 2, 1, 128), ([65, 0, 1, 127, 128, 129], 0, 0, 4, 2, 64), ([31, 33, 63, 2], 5, 40, 3, 3, 128),
-    ([300], 0, 130, 8, 1, 128), ([0, 0, 200, 0], 0, 0, 6, 2, 64), ([257, 255], 1, 1, 4, 4, 128), ([700], 0, 0, 2, 2, 64), ([513, 40], 0, 3, 16, 2, 64), ([0], 9, 8, 2, 1, 64)])
+    ([300], 0, 130, 8, 1, 128), ([0, 0, 200, 0], 0, 0, 6, 2, 64), ([257, 255], 1, 1, 4, 4, 128), ([700], 0, 0, 2, 2, 64), ([513, 40], 0, 3, 16, 2, 64), ([0], 9, 8, 2, 1, 64), ([20], 0, 0, 256, 64, 64), ([9, 8], 0, 2, 64, 8, 128)])
 def test_attention(torch_mod, causal, lens, before, behind, heads, kv, D):
     print("attention", causal, lens, before, behind, heads, kv, D, flush=True)
     rng = np.random.default_rng(sum(lens) + D + heads)
@@ -184,7 +184,7 @@ def test_attention_of_many_sequences(torch_mod, n, most):
 
 
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("seqs,most,heads,kv,D", [(60, 300, 8, 2, 64), (62, 150, 8, 8, 128), (63, 150, 8, 8, 128), (3, 600, 12, 4, 64), (2, 500, 12, 12, 128), (100, 60, 16, 2, 64), (1, 1100, 12, 3, 64)])
+@pytest.mark.parametrize("seqs,most,heads,kv,D", [(60, 300, 8, 2, 64), (62, 150, 8, 8, 128), (63, 150, 8, 8, 128), (3, 600, 12, 4, 64), (2, 500, 12, 12, 128), (100, 60, 16, 2, 64), (1, 1100, 12, 3, 64), (1, 2200, 16, 4, 128)])
 def test_attention_where_the_chip_is_full(torch_mod, causal, seqs, most, heads, kv, D):
     """Launches of one and two groups of wavefronts to a tile, of both gradients apart, and of more sequences than a wavefront has lanes."""
     print("attention", causal, seqs, most, heads, kv, D, flush=True)
@@ -213,6 +213,21 @@ def test_attention_with_flat_and_sharp_scores(torch_mod, size):
     x, gy = storage(x, "bf16"), storage(rng.normal(size=(M, 2 * D)), "bf16")
     b, o = run_attention(torch_mod, x, off, heads, kv, D, True, gy)
     check_attention(o, od.attention(values(x, "bf16"), off, heads, kv, D, True, values(gy, "bf16")), heads, D, 150)
+    b.close()
+
+
+def test_attention_without_its_log_sum_exp(torch_mod):
+    import paper_2203_15980_amd as dl
+    rng = np.random.default_rng(18)
+    off = offsets([70, 33])
+    x = storage(rng.normal(size=(103, 4 * 64)), "bf16")
+    b, o = run_attention(torch_mod, x, off, 2, 1, 64, True)
+    b.d.release(3, dl.EV_EVICT)
+    o["L"].y2 = dl.NO_TENSOR
+    b.d.recompute_segment([o["L"]])
+    assert np.array_equal(values(b.get(2, np.uint16, (103, 128)), "bf16"), o["y"])
+    with pytest.raises(dl.DeltaError):
+        b.d.tensor_ptr(3)
     b.close()
 
 

@@ -273,6 +273,28 @@ def test_two_contexts_on_two_streams_at_once(torch_mod):
         s.b.close()
 
 
+def test_step_large_enough_for_the_second_stream(torch_mod):
+    """Weight gradients of more than 1 GFLOP run on the library's own stream and use the beginning of the workspace that normalisation and attention use the end of: with
+    just the largest need the streams wait for each other, with twice that they do not; the results are the same."""
+    s = Decoder(torch_mod, (1700, 2301, 2500), 3, V=512, FF=640, seed=30)
+    assert "second stream" in s.b.d.backward_kernel(s.backward[9])
+    s.run()
+    want = s.everything()
+    s.check(want)
+    tight = max([s.b.d.backward_workspace(d) for d in s.forward if d.op != s.dl.OP_ROTARY] + [s.b.d.backward_workspace(s.backward[4].fwd)])
+    for b in s.backward:
+        b.workspace_bytes = tight
+    for _ in range(3):
+        for g in s.gw.values():
+            g.fill_(float("nan"))
+        torch_mod.cuda.synchronize()
+        s.run()
+        got = s.everything()
+        for n in want:
+            assert np.array_equal(got[n], want[n]), n
+    s.b.close()
+
+
 # ------------------------------------------------------------------ refusals
 
 def test_refusals_leave_everything_as_it_was(torch_mod):
