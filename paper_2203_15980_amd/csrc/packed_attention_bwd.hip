@@ -194,8 +194,14 @@ __device__ __forceinline__ void gkv_tile(const Args &a, unsigned workgroup, unsi
             if constexpr (!kValuesInLds) vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p + (size_t)a.kv * D * 2 + s * 32));
         }
     }
-    if constexpr (kValuesInLds)
-        Loader<D, W * G, K>(group * W + wave).load(xb + (size_t)first * pitch + (size_t)(a.heads + a.kv + kh) * D * 2, (uint32_t)pitch, r.len - first, lds_of(values));
+    if constexpr (kValuesInLds) {                        // 64 rows from a base of their own: their offsets stay within 32 bits
+        constexpr int kRows = K < 64 ? K : 64;
+#pragma unroll
+        for (int at = 0; at < K; at += kRows)
+            if (first + at < r.len)                      // (the wavefronts of keys behind the last do nothing)
+                Loader<D, W * G, kRows>(group * W + wave).load(xb + (size_t)(first + at) * pitch + (size_t)(a.heads + a.kv + kh) * D * 2, (uint32_t)pitch, r.len - first - at,
+                                                               lds_of(values) + (uint32_t)(at * D * 2));
+    }
     f32x16 gk[DB], gv[DB];
 #pragma unroll
     for (int t = 0; t < DB; ++t)

@@ -167,3 +167,42 @@ def test_attention_beyond_4_gib(torch_mod):
             for got, want in ((t.v["y"][a:b, c[0]], y), (t.v["gx"][a:b, c[0]], ds @ k), (t.v["gx"][a:b, c[1]], ds.t().contiguous() @ q), (t.v["gx"][a:b, c[2]], p.t().contiguous() @ g)):
                 assert ((got.double() - want).abs() <= 0.015 * want.abs().amax()).all()
     t.d.close()
+
+
+def attention_of_some_heads(torch, off, M, H, D, heads, causal, seed):
+    """Both ways with as many key heads as query heads; `heads` of them against 64 bits, the rows of no sequence against zero."""
+    import paper_2203_15980_amd as dl
+    from decoder_util import check_attention
+    from oracle import decoder as od
+    W = 3 * H * D
+    t = Table(torch, x=((M, W), torch.bfloat16), off=((len(off),), torch.int64), y=((M, H * D), torch.bfloat16), lse=((H, M), torch.float32), gy=((M, H * D), torch.bfloat16),
+              gx=((M, W), torch.bfloat16))
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    for n in ("x", "gy"):
+        for lo in range(0, M, 16):
+            part = t.v[n][lo:lo + 16]
+            part.copy_(torch.randn(part.shape, device="cuda:0", generator=g))
+    t.v["off"].copy_(torch.tensor(off))
+    for n in ("y", "lse", "gx"):
+        t.v[n].fill_(float("nan"))
+    i = t.i
+    L = t.layer(dl.OP_ATTENTION_PACKED, M, W, H * D, x=i["x"], res=i["off"], y=i["y"], y2=i["lse"], R=H, S=H, flags=dl.ATTENTION_CAUSAL if causal else 0)
+    t.d.recompute_segment([L])
+    ws = torch.empty(t.d.backward_workspace(L), dtype=torch.uint8, device="cuda:0")
+    t.d.backward_segment([t.bwd(L, i["gy"], i["gx"], ws)])
+    t.d.sync()
+    assert not t.v["gx"][off[-1]:].any() and not t.v["y"][off[-1]:].any() and not t.v["lse"][:, off[-1]:].any()
+    some = lambda n, k: np.concatenate([t.v[n][:, (j * H + h) * D:(j * H + h + 1) * D].double().cpu().numpy() for j in range(k) for h in heads], axis=1)      # noqa: E731
+    x, gy = some("x", 3), some("gy", 1)
+    x[off[-1]:], gy[off[-1]:] = 0, 0
+    o = dict(y=some("y", 1), gx=some("gx", 3), lse=t.v["lse"][list(heads)].double().cpu().numpy())
+    check_attention(o, od.attention(x, np.asarray(off), len(heads), len(heads), D, causal, gy), len(heads), D, int(np.diff(off).max()))
+    t.d.close()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_rows_of_17_megabytes(torch_mod, causal):
+    """A workgroup's 256 rows of values lie further apart than 32 bits reach: 255 rows of 17.66 MB are 4.5e9 bytes."""
+    H, D = 23000, 128
+    assert 255 * 3 * H * D * 2 > 2 ** 32
+    attention_of_some_heads(torch_mod, [0, 255], 256, H, D, (0, 11111, 22999), causal, 40)
