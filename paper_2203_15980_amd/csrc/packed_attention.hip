@@ -203,7 +203,8 @@ const char *packed_attention_check(long long M, long long seqs, int Cin, int Cou
     if (Cin > 1 << 24) return "attention takes rows of at most 16777216 channels";     // 64 of them lie within 32 bits
     if (M <= 0 || M > 0x7FFFFF00LL) return "attention takes 1 to 2147483392 rows";
     if (seqs < 1 || seqs > 0x3FFFFFFFLL) return "offsets must hold one int64 value more than there are sequences";
-    // threads of a launch: 128 queries or keys to 256 threads (fewer where the launch is small), and a workgroup to each sequence and each end
+    // threads of a launch: 128 queries or keys to 256 threads (fewer where the launch is small), and a workgroup to each sequence and each end; with 512 threads to 256
+    // keys at most twice as many: below 2^32
     if ((M / 128 + seqs + 2) * heads * 256 > 0x7FFFFFFFLL) return "too many rows, sequences and heads in one launch";
     return nullptr;
 }

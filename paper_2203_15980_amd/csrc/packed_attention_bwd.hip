@@ -422,7 +422,9 @@ static hipError_t backward(const Args &a, hipStream_t stream) {
     const int gq = groups_of(a.M, a.seqs, a.heads, D), gkv = groups_of(a.M, a.seqs, a.kv * a.splits, D);
     // one launch for both while it has at most two workgroups to a CU (1024 tokens, 12 heads of 64: 38.5 us, two launches 31)
     const long long tiles = (long long)(a.M + 31) / 32 * (a.heads + a.kv * a.splits);
-    if (gq == 4 && gkv == 4 && tiles <= 512 && (long long)(a.heads / a.kv / a.splits) * (a.M + 64) <= kOwn) {
+    // and where its threads, 256 to a slot of either kind, are fewer than 2^32, the most that a launch takes; apart they always are (packed_attention_check)
+    const long long slots = (long long)slots_of(a.M, a.seqs, 32) * (a.heads + a.kv * a.splits);
+    if (gq == 4 && gkv == 4 && tiles <= 512 && slots < 1 << 24 && (long long)(a.heads / a.kv / a.splits) * (a.M + 64) <= kOwn) {
         e = launch_both<D, CAUSAL>(a, stream);
     } else {
         e = gq == 4 ? launch_gq<D, 1, 4, CAUSAL>(a, stream) : gq == 2 ? launch_gq<D, 2, 2, CAUSAL>(a, stream) : launch_gq<D, 4, 1, CAUSAL>(a, stream);

@@ -206,3 +206,16 @@ def test_attention_of_rows_of_17_megabytes(torch_mod, causal):
     H, D = 23000, 128
     assert 255 * 3 * H * D * 2 > 2 ** 32
     attention_of_some_heads(torch_mod, [0, 255], 256, H, D, (0, 11111, 22999), causal, 40)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("M,seqs,D", [(32, 32765, 64), (2048, 32700, 128)])
+def test_attention_of_as_many_sequences_as_a_launch_takes(torch_mod, causal, M, seqs, D):
+    """256 heads: both gradients in one launch would be 32768 x 512 workgroups of 256 threads, 2^32, with 32 rows; with 2048 the gradient of keys and values takes 32710 x 256 of
+    512 threads, 2^32 - 7602176."""
+    H = 256
+    lens = np.zeros(seqs, np.int64)
+    lens[[0, 1, 63, 64, 4095, 4096, seqs // 2, seqs - 2, seqs - 1]] = np.array([5, 1, 0, 2, 3, 1, 4, 6, 7]) if M == 32 else np.array([300, 1, 65, 129, 31, 32, 700, 257, 500])
+    off = np.concatenate([[0], np.cumsum(lens)])
+    assert off[-1] <= M
+    attention_of_some_heads(torch_mod, off.tolist(), M, H, D, (0, 100, 255), causal, 41)
