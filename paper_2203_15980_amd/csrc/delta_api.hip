@@ -1040,9 +1040,8 @@ static delta_status prepare_block(delta_ctx *c, const delta_layer_desc *layers, 
     return DELTA_OK;
 }
 
-// Makes tensor `y` ready to be written on the compute stream: a fresh block, or its own one once
-// nobody else is still reading it.
-static delta_status claim_output(delta_ctx *c, Tensor &ty) {
+// Makes room for an output on the compute stream: a fresh block, or its own one once nobody else is still reading it.
+static delta_status room_for(delta_ctx *c, Tensor &ty) {
     delta_status r;
     if (!ty.resident) {
         if ((r = arena_alloc(c, ty.bytes, S_COMPUTE, &ty.offset)) != DELTA_OK) return r;
@@ -1054,12 +1053,18 @@ static delta_status claim_output(delta_ctx *c, Tensor &ty) {
         if (ty.aux_done)                            // and so may a weight gradient
             HIP_TRY(c, hipStreamWaitEvent(c->stream[S_COMPUTE], ty.aux_done.e, 0));
     }
-    ty.host_valid = false;                          // the host copy, if any, is of older contents
     return DELTA_OK;
 }
 
+// Makes tensor `y` ready to be written on the compute stream.
+static delta_status claim_output(delta_ctx *c, Tensor &ty) {
+    const delta_status r = room_for(c, ty);
+    if (r == DELTA_OK) ty.host_valid = false;       // the host copy, if any, is of older contents
+    return r;
+}
+
 // The same for all outputs of an operator that may have several: y, and at[0], at[1] the addresses of y2 and y3 (null: none).  Where one finds no
-// room, those that were not resident are not resident again: nothing has been computed.
+// room, those that were not resident are not resident again, and host copies count as before: nothing has been computed.
 static delta_status claim_outputs(delta_ctx *c, const delta_layer_desc &L, unsigned char *(&at)[2]) {
     const uint32_t ids[3] = {L.y, L.y2, L.y3};
     bool fresh[3] = {false, false, false};
@@ -1067,7 +1072,7 @@ static delta_status claim_outputs(delta_ctx *c, const delta_layer_desc &L, unsig
         if (j && ids[j] == DELTA_NO_TENSOR) continue;
         Tensor &t = c->tensors[ids[j]];
         fresh[j] = !t.resident;
-        const delta_status r = claim_output(c, t);
+        const delta_status r = room_for(c, t);
         if (r != DELTA_OK) {
             const std::string why = c->err;
             for (int k = 0; k < j; ++k)
@@ -1077,6 +1082,8 @@ static delta_status claim_outputs(delta_ctx *c, const delta_layer_desc &L, unsig
         }
         if (j) at[j - 1] = c->arena + t.offset;
     }
+    for (int j = 0; j < 3; ++j)
+        if (!j || ids[j] != DELTA_NO_TENSOR) c->tensors[ids[j]].host_valid = false;
     return DELTA_OK;
 }
 
