@@ -4,6 +4,9 @@
 //   gz_j = g_lp ([j = id] - p_j) - g_H p_j (z_j - lse + H) + g_lse p_j
 // One pass over the logits: a thread keeps the largest value m so far, s = sum exp(z - m) and w = sum (m - z) exp(z - m), and scales s and w where m
 // grows; threads meet through LDS.  lp = (z - m) - log s and H = log s + w / s: no difference of large numbers.
+//   The gradient takes z_j - lse, which the rounding of lse moves by 2^-24 |lse| for all j, or, where lp is the smaller number, (z_j - z[id]) + lp, off by 2^-24 of
+// |z_j - z[id]| and |lp|: what moves all logits of a row alike moves no probability.  (By lse alone, logits around 500, 10000: p off by 2^-16, 2^-11.)  4 |lp| < |lse|: the two
+// subtractions, lp's own rounding and what it was made of are four of its steps against one of lse's.
 //   A value of -infinity has no weight (z - m is held above -1e30, so that 0 * infinity is not formed).  Where no value has any, lp = lse = -infinity and
 //   H = 0, and the row's gradient is zero.  NaN, or +infinity, makes the row NaN.
 //
@@ -355,8 +358,14 @@ __global__ __launch_bounds__(256) void backward_kernel(Args a, uint32_t chunks) 
         const uint32_t row = (uint32_t)(b / chunks), j = (uint32_t)(b - (uint64_t)row * chunks) * kChunk + threadIdx.x * 8;
         if (j >= a.V) continue;
         const long long id = a.id[row];
-        const float lse = a.y[(uint64_t)2 * a.rows + row];
+        const float lse = a.y[(uint64_t)2 * a.rows + row], lp = a.y[row];
         const bool live = id >= 0 && id < a.V && lse != -__builtin_inff();
+        // log p_j = (z_j - from) + more
+        float from = lse, more = 0.f;
+        if (live && 4.f * fabsf(lp) < fabsf(lse)) {      // (not of infinities and NaN)
+            from = load_one<T>(a.z + ((uint64_t)row * a.V + id) * kEs);
+            more = lp;
+        }
         const float H = a.y[(uint64_t)a.rows + row], g1 = a.gy[row], g2 = a.gy[(uint64_t)a.rows + row], g3 = a.gy[(uint64_t)2 * a.rows + row];
         const uint64_t at = ((uint64_t)row * a.V + j) * kEs;
         const bool whole = j + 8 <= a.V;
@@ -372,7 +381,7 @@ __global__ __launch_bounds__(256) void backward_kernel(Args a, uint32_t chunks) 
         for (int e = 0; e < 8; ++e) {
             float g = 0.f;
             if (live) {
-                const float d = v[e] - lse, p = __builtin_amdgcn_exp2f(d * kLog2e);
+                const float d = (v[e] - from) + more, p = __builtin_amdgcn_exp2f(d * kLog2e);
                 if (p != 0.f) g = p * ((g3 - g1) - g2 * (d + H));
                 if (j + e == (uint32_t)id) g += g1;
             }
