@@ -351,28 +351,36 @@ __global__ __launch_bounds__(1024) void forward_kernel(Args a) {
 }
 
 template <typename T>
+struct Uniform {
+    const __attribute__((address_space(4))) T *p;        // constant memory, as far as the kernel is concerned
+    __device__ __forceinline__ explicit Uniform(const T *at) : p((const __attribute__((address_space(4))) T *)(uintptr_t)at) {}
+    __device__ __forceinline__ T operator[](uint64_t i) const { return p[i]; }
+};
+
+template <typename T>
 __global__ __launch_bounds__(256) void backward_kernel(Args a, uint32_t chunks) {
     constexpr uint32_t kEs = (uint32_t)sizeof(T), kChunk = 256 * 8;
     const uint64_t n = (uint64_t)a.rows * chunks;
     for (uint64_t b = blockIdx.x; b < n; b += gridDim.x) {
         const uint32_t row = (uint32_t)(b / chunks), j = (uint32_t)(b - (uint64_t)row * chunks) * kChunk + threadIdx.x * 8;
         if (j >= a.V) continue;
-        const long long id = a.id[row];
-        const float lse = a.y[(uint64_t)2 * a.rows + row], lp = a.y[row];
+        // The row's numbers, the same for all lanes: nothing here writes them, so scalar loads may bring them.
+        const Uniform<float> y(a.y + row), gy(a.gy + row);
+        const long long id = Uniform<long long>(a.id + row)[0];
+        const float lp = y[0], H = y[a.rows], lse = y[(uint64_t)2 * a.rows], g1 = gy[0], g2 = gy[a.rows], g3 = gy[(uint64_t)2 * a.rows];
         const bool live = id >= 0 && id < a.V && lse != -__builtin_inff();
-        // log p_j = (z_j - from) + more
-        float from = lse, more = 0.f;
-        if (live && 4.f * fabsf(lp) < fabsf(lse)) {      // (not of infinities and NaN)
-            from = load_one<T>(a.z + ((uint64_t)row * a.V + id) * kEs);
-            more = lp;
-        }
-        const float H = a.y[(uint64_t)a.rows + row], g1 = a.gy[row], g2 = a.gy[(uint64_t)a.rows + row], g3 = a.gy[(uint64_t)2 * a.rows + row];
+        asm volatile("" ::"s"(lp));                      // with the others, not behind the branch
         const uint64_t at = ((uint64_t)row * a.V + j) * kEs;
         const bool whole = j + 8 <= a.V;
-        float v[8], o[8];
+        float v[8], o[8], from = lse, more = 0.f;        // log p_j = (z_j - from) + more
         if (live) {
             Raw<T> raw;
-            if (whole) { raw.load(a.z + at); raw.to(v); }
+            if (whole) raw.load(a.z + at);
+            if (4.f * fabsf(lp) < fabsf(lse)) {          // not of infinities and NaN; behind the load above (before it: 4096 x 131072 in bf16 450 us)
+                from = load_one<T>(a.z + ((uint64_t)row * a.V + id) * kEs);
+                more = lp;
+            }
+            if (whole) raw.to(v);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = j + e < a.V ? load_one<T>(a.z + at + e * kEs) : 0.f;
