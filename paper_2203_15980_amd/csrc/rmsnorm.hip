@@ -282,6 +282,7 @@ __global__ __launch_bounds__(1024) void sums_kernel(const float *partial, float 
 // Few rows: one launch for both gradients.  A workgroup owns 64 channels and needs every row's r and mean(g sh), which it makes for itself: all threads go over all values,
 // eight at a time, four threads' sums (a block of 32 channels, never of two rows) go to LDS, eight threads to a row add those; then the same eight make the row's
 // gx of the 64 channels, and the rows' terms of dgamma meet in a fixed order.
+// r is not known yet where g s is summed: s goes in by its block's own power of two, 2^e, and r 2^e multiplies the block's sum, so that what lies between g and r g is in range wherever they are.
 constexpr int kFew = 128;
 constexpr uint32_t kFewValues = 16384;
 template <typename T> constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;              // pieces of a thread on their way
@@ -289,6 +290,7 @@ template <typename T>
 __global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor per_row) {
     constexpr uint32_t kEs = (uint32_t)sizeof(T);
     __shared__ float sums[2][kFewValues / 32];
+    __shared__ int powers[kFewValues / 32];
     __shared__ __align__(16) float parts[16][64];
     const uint32_t lane = threadIdx.x & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t row = threadIdx.x >> 3, ck = blockIdx.x * 8 + (threadIdx.x & 7);
@@ -321,16 +323,22 @@ __global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor pe
             float s[8], g[8], q = 0.f, dot = 0.f;
             u[k].to(s);
             w[k].to(g);
+            uint32_t most = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(s[e]) & 0x7FFFFFFFu);
+            most = max(most, rows::quad_xor1(most));
+            most = max(most, rows::quad_xor2(most));
+            const int power = (int)(most >> 23) - 127;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 q += s[e] * s[e];
-                dot += g[e] * gm[k][e] * s[e];
+                dot += g[e] * gm[k][e] * __builtin_ldexpf(s[e], -power);
             }
             q += rows::dpp<0xB1>(q);
             dot += rows::dpp<0xB1>(dot);
             q += rows::dpp<0x4E>(q);
             dot += rows::dpp<0x4E>(dot);
-            if ((lane & 3) == 0) { sums[0][i / 4] = q; sums[1][i / 4] = dot; }
+            if ((lane & 3) == 0) { sums[0][i / 4] = q; sums[1][i / 4] = dot; powers[i / 4] = power; }
         }
     }
     __syncthreads();
@@ -339,16 +347,18 @@ __global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor pe
         const uint32_t n = a.C / 32;
         float q = 0.f, dot = 0.f;
         if (row < a.rows)
-            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) { q += sums[0][row * n + i]; dot += sums[1][row * n + i]; }
+            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) q += sums[0][row * n + i];
         q += rows::dpp<0xB1>(q);
-        dot += rows::dpp<0xB1>(dot);
         q += rows::dpp<0x4E>(q);
-        dot += rows::dpp<0x4E>(dot);
         q += rows::dpp<0x141>(q);                        // row_half_mirror: the other quad of a lane's eight
-        dot += rows::dpp<0x141>(dot);
         const float over = 1.0f / (float)a.C;
         inverse = 1.0f / sqrtf(q * over + a.eps);
-        mean = dot * over * inverse;
+        if (row < a.rows)
+            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) dot += sums[1][row * n + i] * __builtin_ldexpf(inverse, powers[row * n + i]);
+        dot += rows::dpp<0xB1>(dot);
+        dot += rows::dpp<0x4E>(dot);
+        dot += rows::dpp<0x141>(dot);
+        mean = dot * over;
     }
     float s[8], g[8], dg[8];
     sr.to(s);
