@@ -195,8 +195,8 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * DELTA_OP_ROTARY (bf16 and fp32): x, y [rows][(R + S) D], R rotated heads, then S copied ones, of D channels, a multiple of 16 up to 256.  res: positions,
  * int64 [rows][A], A from 1 to 8 by the tensor's bytes; scale: fp32 frequencies [A][D / 2] in radians a position.  theta_i = sum_a pos_a * scale[a][i]; pair i of a
  * rotated head's channels, (i, i + D / 2) or with DELTA_ROTARY_PAIRS (2 i, 2 i + 1), becomes (u cos theta_i - v sin theta_i, u sin theta_i + v cos theta_i).
- * Frequencies that are zero but for one axis give each pair of channels its axis.  Angles are formed in 64 bits and reduced there: exact to fp32 up to
- * 2^31 radians.
+ * Frequencies that are zero but for one axis give each pair of channels its axis.  Angles are formed and reduced in twice 64 bits: up to 2^31 radians, whatever the
+ * positions, sine and cosine are off by at most 3.5 * 2^-24.
  * DELTA_OP_ATTENTION_PACKED (bf16): x [rows][(R + 2 S) D] = R heads of queries, S of keys, S of values, R a multiple of S, D = 64 or 128; res: offsets, int64,
  * one more than there are sequences (by the tensor's bytes): sequence i is the rows from offset i up to offset i + 1, ascending, possibly none.
  * y [rows][Cout = R D] = softmax(q k^T / sqrt(D)) v over the sequence's rows, with DELTA_ATTENTION_CAUSAL over those up to the query's own; head h reads key head

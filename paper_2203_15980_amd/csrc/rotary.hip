@@ -3,9 +3,10 @@
 //   each rotated head's pair i of channels (u, v) -> (u cos theta - v sin theta, u sin theta + v cos theta); the gradient turns by -theta
 // Pair i is (i, i + D / 2), or (2 i, 2 i + 1) with PAIRS.  Heads behind the rotated ones are copied.
 //
-// Angles.  A position times a frequency is many turns: the products, their sum and the reduction to a turn's fraction are in 64 bits (off by
-// 2^-51 of the angle: 5e-7 at 2^31 radians), then a fraction of an eighth of a turn at most goes to fp32 and into the Taylor polynomials of sine and
-// cosine (to x^9 and x^10: what is left out is below 2e-9).  Computed once a token, by the wavefront that turns its row, and read from LDS for each head.
+// Angles.  A position times a frequency is many turns, of which a fraction counts: 64 bits alone are off by 2^-51 of the angle, 1e-6 at 2^31 radians.  The products,
+// their sum and the turns are held as two 64-bit numbers, the second what the first one's rounding left (the exact product and sum by fma and by Knuth's two-sum; 1 / (2 pi) in
+// two parts), then a fraction of an eighth of a turn at most goes to fp32 and into the Taylor polynomials of sine and cosine (to x^9 and x^10: what is left out is
+// below 2e-9).  Sine and cosine are off by 3.5 * 2^-24 at most.  Computed once a token, by the wavefront that turns its row, and read from LDS for each head.
 //
 // Bound by memory: each value is read and written once.  bf16, 8192 rows of 48 heads of 128, 40 of them rotated, 32 us (201 MB, 6.2 TB/s, part of it from the L2s'
 // shared cache; 45 us, 4.5 TB/s, from HBM); fp32 84 us (403 MB, 4.8 TB/s).
@@ -35,10 +36,30 @@ struct Args {
     float sign;
 };
 
+// A sum of products of whole numbers and fp32 numbers, and what its roundings left.
+struct Angle {
+    double hi = 0.0, lo = 0.0;
+    __device__ __forceinline__ void add(long long pos, double f) {
+#pragma clang fp contract(off)
+        const double top = (double)(int32_t)(pos >> 32) * 4294967296.0, low = (double)(uint32_t)pos;
+        const double n = top + low, rest = low - (n - top);                        // pos = n + rest: top is zero or no smaller than low
+        const double p = n * f, e = __builtin_fma(rest, f, __builtin_fma(n, f, -p));
+        const double sum = hi + p, b = sum - hi;
+        lo += ((hi - (sum - b)) + (p - b)) + e;
+        hi = sum;
+    }
+    __device__ __forceinline__ void turns(double &t, double &rest) const {          // times 1 / (2 pi)
+#pragma clang fp contract(off)
+        constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;
+        t = hi * kTurn;
+        rest = __builtin_fma(lo, kTurn, __builtin_fma(hi, kTurnRest, __builtin_fma(hi, kTurn, -t)));
+    }
+};
+
 // Cosine and sine of an angle in turns: whole quarters aside, an eighth of a turn at most is left.
-__device__ __forceinline__ void turn_of(double t, float &c, float &s) {
+__device__ __forceinline__ void turn_of(double t, double rest, float &c, float &s) {
     const double k = rint(4.0 * t);
-    const float x = (float)(t - 0.25 * k) * 6.28318530717958648f, q = x * x;
+    const float x = (float)((t - 0.25 * k) + rest) * 6.28318530717958648f, q = x * x;
     const float sn = x * (1.0f + q * (-1.66666666666666667e-1f + q * (8.33333333333333333e-3f + q * (-1.98412698412698413e-4f + q * 2.75573192239858907e-6f))));
     const float cs = 1.0f + q * (-0.5f + q * (4.16666666666666667e-2f + q * (-1.38888888888888889e-3f + q * (2.48015873015873016e-5f + q * -2.75573192239858907e-7f))));
     const int n = (int)((long long)k & 3);
@@ -61,11 +82,12 @@ __global__ __launch_bounds__(kWaves * 64) void rotary_kernel(Args a) {
         for (uint32_t i = lane; i < here * half; i += 64) {
             const uint32_t token = (uint32_t)divide((int)i, a.per_half), pair = i - token * half;
             const long long *pos = a.pos + (first + token) * a.axes;
-            double t = 0.0;
-            for (uint32_t x = 0; x < a.axes; ++x) t = __builtin_fma((double)pos[x], (double)a.freq[x * half + pair], t);
-            t *= 0.15915494309189533577;                 // turns
+            Angle angle;
+            for (uint32_t x = 0; x < a.axes; ++x) angle.add(pos[x], (double)a.freq[x * half + pair]);
+            double t, rest;
+            angle.turns(t, rest);
             float c, s;
-            turn_of(t, c, s);
+            turn_of(t, rest, c, s);
             cosine[i] = c;
             sine[i] = a.sign * s;
         }
