@@ -57,13 +57,19 @@ class Event(C.Structure):
 
 
 class LayerDesc(C.Structure):
-    """What is left out is 0: also y2 and y3, which OP_RMSNORM, OP_ROTARY, OP_ATTENTION_PACKED and OP_LOGPROB take as tensor 0 (NO_TENSOR: none)."""
+    """What is left out is 0; y2 and y3, the further outputs of OP_RMSNORM, OP_ROTARY, OP_ATTENTION_PACKED and OP_LOGPROB, NO_TENSOR (none)."""
     _fields_ = [("x", C.c_uint32), ("res", C.c_uint32), ("y", C.c_uint32), ("dtype", C.c_uint32),
                 ("w", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p),
                 ("N", C.c_int32), ("H", C.c_int32), ("W", C.c_int32), ("Cin", C.c_int32),
                 ("Cout", C.c_int32), ("R", C.c_int32), ("S", C.c_int32), ("stride", C.c_int32),
                 ("pad", C.c_int32), ("relu", C.c_uint32), ("op", C.c_uint32), ("eps", C.c_float),
                 ("fuse", C.c_uint32), ("pack", C.c_uint32), ("y2", C.c_uint32), ("y3", C.c_uint32), ("flags", C.c_uint32)]
+
+    def __init__(self, *args, **kw):
+        for at, (name, _) in enumerate(self._fields_):
+            if name in ("y2", "y3") and at >= len(args):
+                kw.setdefault(name, NO_TENSOR)
+        super().__init__(*args, **kw)
 
 
 class BwdDesc(C.Structure):
