@@ -379,7 +379,7 @@ def _prepare_own(case, v):
     if k == "attention":
         for n in ("y", "lse", "gx"):
             if n in i:
-                p.view(n).zero_()                    # rows behind the last sequence stay as they are
+                p.view(n).fill_(math.nan)            # all of them are the operator's to write, also rows of no sequence
         fwd = dl.LayerDesc(op=dl.OP_ATTENTION_PACKED, res=i["off"], y2=i["lse"], y3=none, Cout=wide, R=case["heads"], S=case["kv"],
                            flags=dl.ATTENTION_CAUSAL if case["causal"] else 0, **common)
     elif k == "rmsnorm":
