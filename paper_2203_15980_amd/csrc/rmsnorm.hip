@@ -282,7 +282,7 @@ __global__ __launch_bounds__(1024) void sums_kernel(const float *partial, float 
 // Few rows: one launch for both gradients.  A workgroup owns 64 channels and needs every row's r and mean(g sh), which it makes for itself: all threads go over all values,
 // eight at a time, four threads' sums (a block of 32 channels, never of two rows) go to LDS, eight threads to a row add those; then the same eight make the row's
 // gx of the 64 channels, and the rows' terms of dgamma meet in a fixed order.
-// r is not known yet where g s is summed: s goes in by its block's own power of two, 2^e, and r 2^e multiplies the block's sum, so that what lies between g and r g is in range wherever they are.
+// r is not known yet where g s is summed: s goes in by its block's own power of two, which multiplies the block's sum in 64 bits, so that only mean(g sh) has to be in range.
 constexpr int kFew = 128;
 constexpr uint32_t kFewValues = 16384;
 template <typename T> constexpr int kAtOnce = sizeof(T) == 2 ? 4 : 2;              // pieces of a thread on their way
@@ -345,16 +345,19 @@ __global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor pe
     float inverse = 0.f, mean = 0.f;
     {
         const uint32_t n = a.C / 32;
-        float q = 0.f, dot = 0.f;
+        float q = 0.f;
+        double all = 0.0;                                // sums of g s, for their range
         if (row < a.rows)
-            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) q += sums[0][row * n + i];
+            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) {
+                q += sums[0][row * n + i];
+                all += __builtin_ldexp((double)sums[1][row * n + i], powers[row * n + i]);
+            }
         q += rows::dpp<0xB1>(q);
         q += rows::dpp<0x4E>(q);
         q += rows::dpp<0x141>(q);                        // row_half_mirror: the other quad of a lane's eight
         const float over = 1.0f / (float)a.C;
         inverse = 1.0f / sqrtf(q * over + a.eps);
-        if (row < a.rows)
-            for (uint32_t i = threadIdx.x & 7; i < n; i += 8) dot += sums[1][row * n + i] * __builtin_ldexpf(inverse, powers[row * n + i]);
+        float dot = (float)(all * (double)inverse);
         dot += rows::dpp<0xB1>(dot);
         dot += rows::dpp<0x4E>(dot);
         dot += rows::dpp<0x141>(dot);
