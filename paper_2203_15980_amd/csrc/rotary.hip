@@ -38,14 +38,18 @@ struct Args {
 
 // A sum of products of whole numbers and fp32 numbers, and what its roundings left.
 struct Angle {
-    double hi = 0.0, lo = 0.0;
-    __device__ __forceinline__ void add(long long pos, double f) {
+    double hi, lo;
+    __device__ __forceinline__ Angle(long long pos, double f) {                    // one product
 #pragma clang fp contract(off)
         const double top = (double)(int32_t)(pos >> 32) * 4294967296.0, low = (double)(uint32_t)pos;
         const double n = top + low, rest = low - (n - top);                        // pos = n + rest: top is zero or no smaller than low
-        const double p = n * f, e = __builtin_fma(rest, f, __builtin_fma(n, f, -p));
-        const double sum = hi + p, b = sum - hi;
-        lo += ((hi - (sum - b)) + (p - b)) + e;
+        hi = n * f;
+        lo = __builtin_fma(rest, f, __builtin_fma(n, f, -hi));
+    }
+    __device__ __forceinline__ void add(const Angle &a) {
+#pragma clang fp contract(off)
+        const double sum = hi + a.hi, b = sum - hi;
+        lo += ((hi - (sum - b)) + (a.hi - b)) + a.lo;
         hi = sum;
     }
     __device__ __forceinline__ void turns(double &t, double &rest) const {          // times 1 / (2 pi)
@@ -82,8 +86,8 @@ __global__ __launch_bounds__(kWaves * 64) void rotary_kernel(Args a) {
         for (uint32_t i = lane; i < here * half; i += 64) {
             const uint32_t token = (uint32_t)divide((int)i, a.per_half), pair = i - token * half;
             const long long *pos = a.pos + (first + token) * a.axes;
-            Angle angle;
-            for (uint32_t x = 0; x < a.axes; ++x) angle.add(pos[x], (double)a.freq[x * half + pair]);
+            Angle angle(pos[0], (double)a.freq[pair]);
+            for (uint32_t x = 1; x < a.axes; ++x) angle.add(Angle(pos[x], (double)a.freq[x * half + pair]));
             double t, rest;
             angle.turns(t, rest);
             float c, s;
