@@ -190,7 +190,7 @@ enum { DELTA_FUSE_NONE = 0, DELTA_FUSE_BLOCK = 1, DELTA_FUSE_NO_STORE = 2 };
  * A decoder layer's operators (N * H * W rows, at most 2147483647; y2 and y3 are further outputs, DELTA_NO_TENSOR where there is none):
  * DELTA_OP_RMSNORM (bf16 and fp32, Cin = Cout a multiple of 8 up to 8192): s = x + res, rounded to the storage type and stored in y2; without res s = x and y2
  * is DELTA_NO_TENSOR.  y = s / sqrt(mean(s^2) + eps) * scale over the channels of each row; scale = gamma (fp32, 16-byte aligned), no shift.  The sum of
- * squares is fp32: finite for |s| up to 2^63 / sqrt(Cin).  With `pack`, y3 receives y's checkpoint, the bits that DELTA_OP_PACK8 makes of y;
+ * squares is fp32: finite for |s| up to 2^63 / sqrt(Cin), and to fp32's precision where mean(s^2) + eps is 2^-126 or more.  With `pack`, y3 receives y's checkpoint, the bits that DELTA_OP_PACK8 makes of y;
  * without, y3 is DELTA_NO_TENSOR.
  * DELTA_OP_ROTARY (bf16 and fp32): x, y [rows][(R + S) D], R rotated heads, then S copied ones, of D channels, a multiple of 16 up to 256.  res: positions,
  * int64 [rows][A], A from 1 to 8 by the tensor's bytes; scale: fp32 frequencies [A][D / 2] in radians a position.  theta_i = sum_a pos_a * scale[a][i]; pair i of a
@@ -398,7 +398,8 @@ delta_status delta_set_skip_copies(delta_ctx *ctx, int32_t skip);
  *   DELTA_OP_ATTENTION_PACKED (bf16) gx, all of it: of queries, keys and values, the latter two summed over the heads that read them in a fixed order; zero in rows of
  *                      no sequence.  Needs fwd.x, fwd.res (offsets), fwd.y and fwd.y2 (log-sum-exp) resident, and a workspace.  No gw, no gx_add.
  *   DELTA_OP_LOGPROB   (bf16 and fp32) gy fp32 [3][rows], the gradients of the log probability, the entropy and the log-sum-exp: gx_j = gy_0 ([j = id] - p_j)
- *                      - gy_1 p_j (log p_j + entropy) + gy_2 p_j; zero in rows without a token or without weight.  Needs fwd.x, fwd.res (ids) and fwd.y
+ *                      - gy_1 p_j (log p_j + entropy) + gy_2 p_j; zero in rows without a token or without weight.  What moves all of a row's logits alike costs p no
+ *                      precision, but where the token itself lies as far below the others: p is off by 2^-24 of the smaller of |log-sum-exp| and 4 |log probability|.  Needs fwd.x, fwd.res (ids) and fwd.y
  *                      resident.  No gradient of the alternatives, no gw, no gx_add.
  *   DELTA_OP_RELU      (bf16) gx = gy * [y > 0] on the stored output; needs fwd.y resident; gpre = gy.
  *   the stem           (DELTA_OP_CONV, 7x7, stride 2, pad 3, 3 -> 64 channels, bf16): weight gradient only

@@ -16,8 +16,9 @@
 // wavefront's lanes takes the logits one by one instead.  Order: value (a NaN above all, -0 as 0), of equal ones the lowest index: exact, from the logits'
 // own bits.
 //
-// Bound by memory where there are many rows: 4096 x 131072 in bf16 (1.07 GB) forward 208 to 234 us (4.6 to 5.2 TB/s), gradient 395 to 430 us (2.15 GB, 5.0 to
-// 5.4 TB/s).  333 x 50001 in fp32 with 5 alternatives 24 us (67 MB), gradient 21 us; one row of 30522 with 20 alternatives 8.6 to 10.6 us: latency.
+// Bound by memory where there are many rows: 4096 x 131072 in bf16 (1.07 GB) forward 185 to 247 us (4.3 to 5.8 TB/s), gradient 355 to 402 us (2.15 GB, 5.3 to
+// 6.0 TB/s), the least in calls of one kind after one another, the most where they take turns.  333 x 50001 in fp32 with 5 alternatives 24 us (67 MB), gradient 21 us (logits around
+// 10000: 23); one row of 30522 with 20 alternatives 8.1 to 10.4 us: latency.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -417,6 +418,14 @@ hipError_t launch_logprob(const void *z, const void *id, float *y, float *best, 
     lpr::Args a = {};
     a.z = static_cast<const unsigned char *>(z); a.id = static_cast<const long long *>(id); a.y = y; a.best = best; a.which = which;
     a.rows = (uint32_t)rows; a.V = (uint32_t)V; a.K = (uint32_t)K;
+    // Wavefronts to a row, by its length alone.  us with 1, 4 and 16 in bf16, without alternatives, then with 5 (fp32: the same order but where all wait for memory):
+    //   V        1 row                             333 rows                            4096 rows
+    //   2048     3.5, 3.2, 3.2   7.7, 4.8, 4.8     3.9, 3.6, 4.4   8.8, 5.5, 8.5       5.8, 7.8, 18.7    13.3, 15.4, 58
+    //   4095     4.3, 3.3, 3.7   9.7, 5.3, 4.7     4.9, 4.1, 4.7   10.7, 6.3, 8.9      9.5, 11.6, 22.5   18.8, 20.7, 65
+    //   8191     5.9, 3.6, 3.6   11.9, 6.0, 5.0    6.5, 4.7, 5.1   14.0, 7.8, 9.7      15.1, 19.1, 27.9  27.2, 29.0, 72
+    //   16383    9.3, 4.6, 4.3   17.5, 8.2, 6.0    10.1, 5.9, 6.4  20.3, 10.2, 12.2    24.8, 28.2, 40.1  43.1, 39.9, 94
+    //   32768    15.8, 6.0, 5.2  27.8, 11.1, 7.6   17.2, 8.3, 8.3  32.3, 14.6, 14.8    44.2, 45.0, 55.2  75.4, 62.4, 118
+    // A compromise: few rows would have more wavefronts at each length, thousands of rows fewer, which a rule by rows too could give.
     const uint32_t waves = V >= 16 * 1024 ? 16 : V >= 4096 ? 4 : 1;
     auto run = [&](auto kernel) { kernel<<<dim3(a.rows < 65536u ? a.rows : 65536u), dim3(waves * 64), 0, stream>>>(a); };
     if (bf16) { if (K) run(lpr::forward_kernel<rows::bf16, true>); else run(lpr::forward_kernel<rows::bf16, false>); }

@@ -12,10 +12,10 @@
 // Bound by the SIMDs: a block of 64 keys takes a wavefront 2 D * 64 * 32 * 2 operations, 1024 cycles of the matrix unit with D = 128, and about as many of the vector unit (an exponential,
 // a multiply-add, an addition, half a maximum and half a conversion a score), which overlap little; and by power, as the clock falls to 1.8 to 1.9 GHz.  8192
 // tokens, 32 heads over 8 of 128, causal: 540 to 595 us, 920 to 1020 TFLOP/s (a large matrix product reaches 1175 here; the matrix units 54 % busy, no bank conflicts);
-// 9 packed sequences of up to 1531, 16 heads over 2 of 128 50 us (630 TFLOP/s); 32 of up to 512, 12 heads of 64, not causal 27 us (360 TFLOP/s: the vector unit's work
+// 9 packed sequences of up to 1531, 16 heads over 2 of 128 50 to 54 us (580 to 630 TFLOP/s); 32 of up to 512, 12 heads of 64, not causal 27 us (360 TFLOP/s: the vector unit's work
 // is the same for half the products); 77 tokens 4.9 us: latency.
-// Tried and not kept: the next block's scores under this one's exponentials (8192 tokens 552 and 561 us, 4096 157 and 152, 2048 tokens of 8 heads 30 and 29), a wavefront's
-// priority raised around its products (the same), two wavefronts' tiles from padded rows through registers (704 us).
+// Tried with heads of 128 and not kept: the next block's scores under this one's exponentials (8192 tokens 552 and 561 us, 4096 157 and 152, 2048 tokens of 8 heads 30 and 29), a
+// wavefront's priority raised around its products (the same), two wavefronts' tiles from padded rows through registers (704 us).  Heads of 64, which leave more registers: not measured.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -7,7 +7,7 @@
 //   gq: as the forward kernel, a lane owns a query: S^T = K Q^T, dP^T = V gO^T, gQ^T += K^T dS^T.
 //   gk, gv: a lane owns a key: S = Q K^T, dP = gO V^T, gV^T += gO^T P, gK^T += Q^T dS; queries and their gradients come through LDS.
 // p and ds are rounded to bf16 before they multiply, and delta reads ctx as it was stored, in bf16: three roundings of about the size of the result's own (0.0017 of the gradient
-// each; together 0.0024 to 0.0027 against 64 bits); all sums are fp32.
+// each; together 0.0024 to 0.0026 against 64 bits with sequences of hundreds and more, up to 0.0031 with tens, 0.0036 with two rows); all sums are fp32.
 //
 // Bound by the SIMDs as the forward kernel is.  8192 tokens, 32 heads over 8 of 128, causal: gq 735 to 770 us (825 GFLOP: 1070 to 1120 TFLOP/s, the matrix units 61 to 64 % busy), gk and gv
 // 1010 to 1080 us (1100 GFLOP: 1020 to 1090 TFLOP/s) and 25 for the parts; counted as five products 800 TFLOP/s.  32 sequences of up to 512, 12 heads of 64, not causal: 36 and 50 us.

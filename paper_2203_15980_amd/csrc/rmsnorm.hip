@@ -8,8 +8,9 @@
 //
 // Bound by memory: forward with residual and checkpoint 9.03 bytes a value in bf16, backward with gx_add 8.  A wavefront owns a row up to 2048 channels, a
 // workgroup beyond (eight channels a thread); the row stays in registers from its load to its store.  us, rows one after another from HBM: 8192 x 4096 in bf16
-// forward with residual and int8 checkpoint 52 (303 MB, 5.8 TB/s), gradients with gx_add 46 (268 MB, 5.8 TB/s); fp32 forward 107 (5.3 TB/s), gradients 101
-// (5.3 TB/s); 16384 x 768 in bf16 forward 16, gradients 22 (their operands partly from the shared cache); 77 x 768 3.4 and 6.3: launches.
+// forward with residual and int8 checkpoint 52 (303 MB, 5.8 TB/s), gradients with gx_add 60 to 62 (268 MB, 4.3 to 4.5 TB/s; 46 to 49 where calls follow each other and find
+// operands in the shared cache); fp32 forward without a checkpoint 87 to 89 (537 MB, 6.1 TB/s), gradients 106 to 108 (5.0 TB/s); 16384 x 768 in bf16 forward 16, gradients 19
+// (their operands partly from the shared cache); 77 x 768 3.4 and 6.3: launches.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(1024) void few_kernel(Args a, float *gw, Divisor pe
     for (int w = 0; w < 16; ++w) sum += parts[w][threadIdx.x];
     gw[c] = sum;
 }
-// us with gx_add, bf16: 1 x 4096 3.8, 128 x 64 4.1, two launches 6.2 whatever the size up to 77 x 768, which takes 7.0 like this: a workgroup reads everything.
+// us with gx_add, bf16: 1 x 4096 4.3, 128 x 64 4.6, two launches 6.2 whatever the size up to 77 x 768, which takes 7.0 like this: a workgroup reads everything.
 constexpr bool few_rows(uint64_t rows, uint64_t C) { return rows <= kFew && rows * C <= kFewValues && C % 32 == 0; }
 
 // Workgroups of the backward launch, a partial sum of dgamma to each.  A row to a workgroup: two at least, whose loads go out together, and the partial sums are half as many (us

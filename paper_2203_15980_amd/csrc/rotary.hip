@@ -8,8 +8,8 @@
 // two parts), then a fraction of an eighth of a turn at most goes to fp32 and into the Taylor polynomials of sine and cosine (to x^9 and x^10: what is left out is
 // below 2e-9).  Sine and cosine are off by 3.5 * 2^-24 at most.  Computed once a token, by the wavefront that turns its row, and read from LDS for each head.
 //
-// Bound by memory: each value is read and written once.  bf16, 8192 rows of 48 heads of 128, 40 of them rotated, 32 us (201 MB, 6.2 TB/s, part of it from the L2s'
-// shared cache; 45 us, 4.5 TB/s, from HBM); fp32 84 us (403 MB, 4.8 TB/s).
+// Bound by memory: each value is read and written once.  bf16, 8192 rows of 48 heads of 128, 40 of them rotated, 33 us (201 MB, 6.1 TB/s, part of it from the L2s'
+// shared cache; 40 to 45 us, 4.5 to 5.0 TB/s, from HBM); fp32 84 us (403 MB, 4.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -71,7 +71,7 @@ __device__ __forceinline__ void turn_of(double t, double rest, float &c, float &
     s = n == 0 ? sn : n == 1 ? cs : n == 2 ? -sn : -cs;
 }
 
-// A wavefront takes `tokens` rows at a time: as many as have 64 pieces together (30000 rows of 96 channels 4.7 us; one row at a time 9.4).
+// A wavefront takes `tokens` rows at a time: as many as have 64 pieces together (30000 rows of 96 channels 6.6 us; one row at a time 10.4).
 template <typename T, bool PAIRS>
 __global__ __launch_bounds__(kWaves * 64) void rotary_kernel(Args a) {
     constexpr uint32_t kEs = (uint32_t)sizeof(T);
