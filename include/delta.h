@@ -237,7 +237,7 @@ typedef struct {
     uint32_t pack;             /* DELTA_PACK_*: the format of y (DELTA_OP_PACK8) or of x (DELTA_OP_UNPACK8; in a backward descriptor
                                   also DELTA_OP_LAYERNORM and linear layers) or of y3 (DELTA_OP_RMSNORM); 0 everywhere else */
     uint32_t y2, y3;           /* further outputs of DELTA_OP_RMSNORM, DELTA_OP_ATTENTION_PACKED and DELTA_OP_LOGPROB, DELTA_NO_TENSOR for none (DELTA_OP_ROTARY:
-                                  both); other operators do not look at them */
+                                  both; 0, as in a cleared descriptor, is tensor 0); other operators do not look at them */
     uint32_t flags;            /* DELTA_ATTENTION_CAUSAL, DELTA_ROTARY_PAIRS; 0 everywhere else */
 } delta_layer_desc;
 
